@@ -490,6 +490,106 @@ int ecospa_embed_bwd(ecospa_ctx* ctx, int T, int d, int vocab, int dtype, const 
 int ecospa_xent(ecospa_ctx* ctx, int T, int V, int dtype, const void* logits, long long ldl, const long long* targets,
                 void* dlogits, long long ldd, float* row_loss, float* loss);
 
+/* ------------------------------------------------------------------------------------------
+ * Serving a compact model token by token.  The keys and values of the tokens that a request has behind it are kept in a cache of
+ * compact heads (only the kept dims of a head are stored); a prefix that all requests of a batch share - a system prompt, a
+ * document - is kept once for all of them.  bf16 storage, as the attention block; fp32 arithmetic; results repeat bit for bit.
+ *
+ * ecospa_cache: B requests, each with `lens[b]` keys of its own (device int32, read when the kernels run; a length outside
+ * [0, own_max] counts as the nearer bound), the tokens of the present call among them: the L new tokens of a call are the last L
+ * keys.  Own row j of request b and key/value head g lies at k + b*k_sb + g*k_sh + j*k_st (kp_qk elements) and v + b*v_sb + g*v_sh
+ * + j*v_st (kp_vo elements); prefix row j at pk + g*pk_sh + j*pk_st and pv + g*pv_sh + j*pv_st - e.g. the K and V columns of the
+ * saved qkv rows of an ecospa_coupled_fwd over the prefix, or a cache of one request that ecospa_cache_append filled.  Strides in
+ * elements, multiples of 8, at most 2^25 - 1 between rows; pointers 16-byte aligned.  kp_qk, kp_vo: multiples of 16 up to 128.
+ * own_max: no request holds more than this many own keys (0: none has any); it only bounds the work, cap bounds the memory.
+ * Rows at and beyond lens[b] are never read.
+ * Common errors, before any launch: ERR_NULL; ERR_DTYPE (dtype other than ECOSPA_BF16); ERR_SHAPE (B, h_kv, cap, L < 1; h_kv does
+ * not divide h; widths; own_max outside [0, cap]; P < 0; scale not a positive number; row strides; B * h_kv > 65535, B * L * h >
+ * 2^30); ERR_ALIGN; ERR_WORKSPACE.
+ * ------------------------------------------------------------------------------------------ */
+typedef struct {
+  int dtype, B, h, h_kv, kp_qk, kp_vo;
+  int cap;                   /* rows of a request's own cache                                  */
+  int own_max;               /* upper bound on lens                                            */
+  int P;                     /* rows of the shared prefix, 0: none                             */
+  float scale;               /* softmax scale (1/sqrt(original d_h))                           */
+  void *k, *v;
+  long long k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  const void *pk, *pv;
+  long long pk_sh, pk_st, pv_sh, pv_st;
+  const int* lens;           /* device int32[B]                                                */
+} ecospa_cache;
+
+/* The L new tokens of every request go into its cache.  qkv: rows [B*L, h*kp_qk | h_kv*kp_qk | h_kv*kp_vo] as the projection writes
+ * them (leading dimension ld_qkv), token t of request b in row b*L + t.  Its key and value become own row lens[b] - L + t.  With
+ * rope_cos/rope_sin (float[h_kv, L_tab, kp_qk/2], ecospa_rope_table: the angles of the KEPT rotary blocks of every head) queries and
+ * keys are turned by the angles of position pos[b] + t (pos: device int32[B], the position of the first new token - it goes on
+ * counting when keys were evicted); NULL: none.  q [B*L, h*kp_qk] (ld_q) receives the queries; NULL (without tables only): not
+ * wanted, they are the first columns of qkv; q may be qkv itself with ld_q = ld_qkv.  weights (float[B, h_kv, cap], NULL: none): the
+ * new rows' entries are set to zero.  A token whose row is outside [0, cap) or whose position is outside the tables is not put
+ * into the cache, and its query is zero.  Errors also: ERR_NULL (one table only; tables without pos or q), ERR_SHAPE (L_tab < 1,
+ * ld_qkv, ld_q below the row). */
+int ecospa_cache_append(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int L, const void* qkv, long long ld_qkv,
+                        const int* pos, const float* rope_cos, const float* rope_sin, int L_tab, void* q, long long ld_q,
+                        float* weights);
+
+/* Attention of the L new tokens of every request over the shared prefix and the request's own cache: query (b, t) sees all P
+ * prefix keys and the own keys j < lens[b] - L + 1 + t.  Prefix keys are read once for all requests.  q [B*L, h*kp_qk] (ld_q),
+ * o [B*L, h*kp_vo] (ld_o); query head i uses key/value head i / (h / h_kv).  lse (float[B, h, L], NULL: not wanted) receives
+ * log sum exp of the scaled scores.  A query that sees no key has o = 0 and lse = -inf.
+ * weights_out (float[B, h_kv, cap], NULL: not wanted): for every own key j < lens[b], weights_in (same layout, may be weights_out
+ * itself; NULL: zeros) plus the probabilities that the queries of its group gave it: the accumulated attention weight that
+ * ecospa_cache_evict goes by.  Entries beyond lens[b] are left as they are.
+ * Keys a query does not see carry no weight, but the values of the request's other new tokens have to be finite numbers.
+ * Workspace: ecospa_prefix_attn_workspace_bytes (host-only query; 0 when none is needed or on bad input). */
+size_t ecospa_prefix_attn_workspace_bytes(const ecospa_cache* cache /*host*/, int L);
+int ecospa_prefix_attn(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int L, const void* q, long long ld_q, void* o,
+                       long long ld_o, float* lse, const float* weights_in, float* weights_out);
+
+/* Own caches cut down to `keep` keys per request and key/value head, out of place: the last `recent` keys stay, and of the others
+ * the keep - recent with the largest accumulated weight (float[B, h_kv, cap]; order as ecospa_select_topk: equal weights keep the
+ * lower row, NaN ranks below every number); a request with no more than `keep` keys keeps them all.  Kept rows keep their order.
+ * dst (its k, v, strides and cap >= keep; B, h_kv and widths as src; must not overlap it): receives the kept rows; weights_out
+ * (float[B, h_kv, dst->cap], NULL: not wanted) their weights, lens_out (int32[B]) the new lengths min(lens[b], keep), idx
+ * (int32[B, h_kv, keep], NULL: not wanted) the kept rows' numbers, then -1.  Other rows of dst are left as they are.
+ * Errors also: ERR_K (keep < 1, recent outside [0, keep], dst->cap < keep).  Workspace (idx NULL only): B * h_kv * keep int32. */
+int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src /*host*/, const float* weights, int keep, int recent,
+                       const ecospa_cache* dst /*host*/, int* lens_out, float* weights_out, int* idx);
+
+/* Penalties for the tokens of a history, biases, temperature and masks on logits, with the best token of every row.  For row b and
+ * token v with c occurrences among the first history_len[b] entries of history row b (int32, ids outside [0, V) are skipped):
+ *   c > 0:  x <- x / repetition[b] if x > 0, else x * repetition[b];   x <- x - frequency[b] * c - presence[b]
+ *   x <- x + sum of bias[b][i] over the entries with bias_ids[b][i] == v (in the order of i);   x <- x / temperature[b]
+ *   x <- -inf where bit v % 32 of word v / 32 of mask row mask_row[b] is 0 (mask_row[b] outside [0, n_masks): no mask).
+ * out (dtype out_dtype, may be the logits themselves with the same type and ld; NULL: not wanted) receives x rounded once, pick
+ * (int32[B], NULL: not wanted) the lowest token with the largest x before rounding (NaN ranks below every number; -1: every token
+ * is -inf or NaN) and lse (float[B], NULL: not wanted) log sum exp x.  Each of the parameter arrays may be NULL (1 for repetition and
+ * temperature, 0 for the others).  dtype ECOSPA_F32 or ECOSPA_BF16, fp32 arithmetic.
+ * Errors: ERR_NULL; ERR_DTYPE; ERR_SHAPE (B, V < 1, B > 65535, V > 2^24, leading dimensions, n_bias outside [0, 1023], history rows
+ * of 2^22 entries and more); ERR_ALIGN (logits, out: 16 bytes, leading dimensions % 8); ERR_WORKSPACE
+ * (ecospa_logits_workspace_bytes). */
+typedef struct {
+  int B, V, dtype, out_dtype;
+  const void* logits;
+  void* out;
+  long long ld, ld_out;
+  const int* history;          /* [B, ld_history] or NULL */
+  const int* history_len;      /* int32[B]; NULL: all of ld_history */
+  int ld_history;
+  int n_bias;                  /* entries of a bias row, 0: none */
+  const float *repetition, *frequency, *presence, *temperature;      /* float[B] or NULL */
+  const int* bias_ids;         /* [B, n_bias]; ids outside [0, V) are skipped */
+  const float* bias;           /* [B, n_bias] */
+  const unsigned* mask;        /* [n_masks, ld_mask] words or NULL */
+  const int* mask_row;         /* int32[B] */
+  long long ld_mask;           /* words, at least ceil(V / 32) */
+  int n_masks;
+  int* pick;
+  float* lse;
+} ecospa_logits;
+size_t ecospa_logits_workspace_bytes(int B, int V);
+int ecospa_logits_process(ecospa_ctx* ctx, const ecospa_logits* args /*host*/);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,6 +32,8 @@ EXPORTS = (
     "ecospa_coupled_score_static", "ecospa_coupled_score_static_max_bytes",
     "ecospa_score_select", "ecospa_compact_batch_rope",
     "ecospa_norm_fwd", "ecospa_norm_bwd", "ecospa_norm_bwd_workspace_bytes", "ecospa_embed_fwd", "ecospa_embed_bwd", "ecospa_xent",
+    "ecospa_cache_append", "ecospa_prefix_attn", "ecospa_prefix_attn_workspace_bytes", "ecospa_cache_evict",
+    "ecospa_logits_process", "ecospa_logits_workspace_bytes",
 )
 NORM_RMS, NORM_LAYER = 0, 1
 
@@ -98,6 +100,22 @@ class AdamwHyper(C.Structure):
 class Saved(C.Structure):
     _fields_ = [("qkv", C.c_void_p), ("o", C.c_void_p), ("lse", C.c_void_p), ("hpre", C.c_void_p),
                 ("act", C.c_void_p)]
+
+
+class Cache(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("B", C.c_int), ("h", C.c_int), ("h_kv", C.c_int), ("kp_qk", C.c_int), ("kp_vo", C.c_int),
+                ("cap", C.c_int), ("own_max", C.c_int), ("P", C.c_int), ("scale", C.c_float), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_sb", C.c_longlong), ("k_sh", C.c_longlong), ("k_st", C.c_longlong), ("v_sb", C.c_longlong), ("v_sh", C.c_longlong),
+                ("v_st", C.c_longlong), ("pk", C.c_void_p), ("pv", C.c_void_p), ("pk_sh", C.c_longlong), ("pk_st", C.c_longlong),
+                ("pv_sh", C.c_longlong), ("pv_st", C.c_longlong), ("lens", C.c_void_p)]
+
+
+class Logits(C.Structure):
+    _fields_ = [("B", C.c_int), ("V", C.c_int), ("dtype", C.c_int), ("out_dtype", C.c_int), ("logits", C.c_void_p), ("out", C.c_void_p),
+                ("ld", C.c_longlong), ("ld_out", C.c_longlong), ("history", C.c_void_p), ("history_len", C.c_void_p), ("ld_history", C.c_int),
+                ("n_bias", C.c_int), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("temperature", C.c_void_p),
+                ("bias_ids", C.c_void_p), ("bias", C.c_void_p), ("mask", C.c_void_p), ("mask_row", C.c_void_p), ("ld_mask", C.c_longlong),
+                ("n_masks", C.c_int), ("pick", C.c_void_p), ("lse", C.c_void_p)]
 
 
 class Grads(C.Structure):
@@ -198,6 +216,18 @@ def load() -> C.CDLL:
     lib.ecospa_xent.argtypes = [vp, ci, ci, ci, vp, ll, vp, vp, ll, vp, vp]
     lib.ecospa_xent.restype = ci
     lib.ecospa_hbm_probe.restype = ci
+    lib.ecospa_cache_append.argtypes = [vp, C.POINTER(Cache), ci, vp, ll, vp, vp, vp, ci, vp, ll, vp]
+    lib.ecospa_cache_append.restype = ci
+    lib.ecospa_prefix_attn.argtypes = [vp, C.POINTER(Cache), ci, vp, ll, vp, ll, vp, vp, vp]
+    lib.ecospa_prefix_attn.restype = ci
+    lib.ecospa_prefix_attn_workspace_bytes.argtypes = [C.POINTER(Cache), ci]
+    lib.ecospa_prefix_attn_workspace_bytes.restype = sz
+    lib.ecospa_cache_evict.argtypes = [vp, C.POINTER(Cache), vp, ci, ci, C.POINTER(Cache), vp, vp, vp]
+    lib.ecospa_cache_evict.restype = ci
+    lib.ecospa_logits_process.argtypes = [vp, C.POINTER(Logits)]
+    lib.ecospa_logits_process.restype = ci
+    lib.ecospa_logits_workspace_bytes.argtypes = [ci, ci]
+    lib.ecospa_logits_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -220,6 +250,48 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def round_up(x: int, m: int) -> int:
     return (x + m - 1) // m * m
+
+
+class KvCache:
+    """A batch's own key/value caches on compact heads, with the prefix that its requests share (ecospa_cache).
+
+    k: [B, h_kv, cap, kp_qk], v: [B, h_kv, cap, kp_vo] (bf16, last dim dense, other strides free); lens: int32 [B], own keys of every
+    request; h query heads; scale: the softmax scale; pk: [h_kv, P, kp_qk], pv: [h_kv, P, kp_vo] or None.  own_max (default: cap): no
+    request holds more keys than this, a smaller bound saves work; it may be set between calls.  The object keeps the tensors alive;
+    their contents, lens included, are read when the kernels run."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, h: int, scale: float, pk: Optional[torch.Tensor] = None,
+                 pv: Optional[torch.Tensor] = None, own_max: Optional[int] = None):
+        Bsz, h_kv, cap, kq = k.shape
+        assert v.shape[:3] == k.shape[:3] and v.dtype == k.dtype and k.stride(3) == 1 and v.stride(3) == 1
+        assert lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == Bsz and (pk is None) == (pv is None)
+        self.k, self.v, self.lens, self.pk, self.pv = k, v, lens, pk, pv
+        self.B, self.h, self.h_kv, self.cap, self.kq, self.kv = Bsz, h, h_kv, cap, kq, v.shape[3]
+        P, prefix = 0, (0, 0, 0, 0)
+        if pk is not None:
+            P = pk.shape[1]
+            assert pk.shape == (h_kv, P, kq) and pv.shape == (h_kv, P, self.kv) and pk.dtype == k.dtype and pv.dtype == k.dtype
+            assert pk.stride(2) == 1 and pv.stride(2) == 1
+            prefix = (pk.stride(0), pk.stride(1), pv.stride(0), pv.stride(1))
+        self.desc = Cache(dtype_code(k.dtype), Bsz, h, h_kv, kq, self.kv, cap, cap if own_max is None else own_max, P, scale, k.data_ptr(),
+                          v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.stride(0), v.stride(1), v.stride(2),
+                          _ptr(pk) if P else None, _ptr(pv) if P else None, *prefix, lens.data_ptr())
+        self._ref = C.byref(self.desc)
+        self._need = {}
+
+    @property
+    def own_max(self) -> int:
+        return self.desc.own_max
+
+    @own_max.setter
+    def own_max(self, n: int):
+        self.desc.own_max = n
+
+    def workspace_bytes(self, L: int) -> int:
+        key = (L, self.desc.own_max)
+        if key not in self._need:
+            self._need[key] = load().ecospa_prefix_attn_workspace_bytes(self._ref, L)
+        return self._need[key]
 
 
 class Context:
@@ -592,6 +664,90 @@ class Context:
                                          _ptr(dlogits), 0 if dlogits is None else dlogits.stride(0), row_loss.data_ptr(),
                                          loss.data_ptr()), "ecospa_xent")
         return loss
+
+    # ---- serving -------------------------------------------------------------------------------
+    def _tokens(self, cache: KvCache, x: torch.Tensor) -> int:
+        assert x.dim() == 2 and x.stride(1) == 1 and x.dtype == torch.bfloat16 and x.shape[0] % cache.B == 0
+        return x.shape[0] // cache.B
+
+    def _weights_ok(self, cache: KvCache, w: Optional[torch.Tensor], cap: int) -> bool:
+        return w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.shape == (cache.B, cache.h_kv, cap))
+
+    def ecospa_cache_append(self, cache: KvCache, qkv: torch.Tensor, pos: Optional[torch.Tensor] = None, rope=None,
+                            q: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None):
+        """The L = rows / B new tokens of every request (rows of the projection: Q | K | V columns) become the last L rows of its cache;
+        cache.lens counts them already.  rope: (cos, sin) [h_kv, L_tab, kp_qk / 2] turns queries (into q) and keys by the angles of
+        positions pos[b] + t; weights [B, h_kv, cap]: the new rows' accumulated weights are set to zero."""
+        L = self._tokens(cache, qkv)
+        assert qkv.shape[1] >= (cache.h + cache.h_kv) * cache.kq + cache.h_kv * cache.kv
+        assert q is None or (self._tokens(cache, q) == L and q.shape[1] >= cache.h * cache.kq)
+        assert pos is None or (pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == cache.B)
+        assert self._weights_ok(cache, weights, cache.cap)
+        cos, sin = rope if rope is not None else (None, None)
+        if cos is not None:
+            assert cos.shape == sin.shape and cos.dtype == sin.dtype == torch.float32 and cos.is_contiguous() and sin.is_contiguous()
+            assert cos.shape[0] == cache.h_kv and cos.shape[2] == cache.kq // 2
+        self._check(self.lib.ecospa_cache_append(self.h, cache._ref, L, qkv.data_ptr(), qkv.stride(0), _ptr(pos), _ptr(cos), _ptr(sin),
+                                                 0 if cos is None else cos.shape[1], _ptr(q), 0 if q is None else q.stride(0),
+                                                 _ptr(weights)), "ecospa_cache_append")
+
+    def ecospa_prefix_attn(self, cache: KvCache, q: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                           weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """o [B*L, h * kp_vo] = attention of the new tokens' queries q [B*L, h * kp_qk] over the shared prefix and the own caches; lse
+        float32 [B, h, L]; weights_out [B, h_kv, cap] = weights (None: zeros) + what every own key received."""
+        L = self._tokens(cache, q)
+        assert self._tokens(cache, o) == L and q.shape[1] >= cache.h * cache.kq and o.shape[1] >= cache.h * cache.kv
+        assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == cache.B * cache.h * L)
+        assert self._weights_ok(cache, weights, cache.cap) and self._weights_ok(cache, weights_out, cache.cap)
+        self.reserve(cache.workspace_bytes(L))
+        self._check(self.lib.ecospa_prefix_attn(self.h, cache._ref, L, q.data_ptr(), q.stride(0), o.data_ptr(), o.stride(0), _ptr(lse),
+                                                _ptr(weights), _ptr(weights_out)), "ecospa_prefix_attn")
+        return o
+
+    def ecospa_cache_evict(self, cache: KvCache, weights: torch.Tensor, keep: int, recent: int, k_out: torch.Tensor, v_out: torch.Tensor,
+                           lens_out: torch.Tensor, weights_out: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None):
+        """The last `recent` rows of every cache and, of the others, those with the largest weights, `keep` in all, gathered in order into
+        k_out, v_out [B, h_kv, cap_out, kp]; lens_out int32 [B]; weights_out float32 [B, h_kv, cap_out]; idx int32 [B, h_kv, keep]."""
+        assert k_out.shape[:2] == (cache.B, cache.h_kv) and self._weights_ok(cache, weights, cache.cap)
+        assert self._weights_ok(cache, weights_out, k_out.shape[2]) and lens_out.data_ptr() != cache.lens.data_ptr()
+        assert idx is None or (idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape == (cache.B, cache.h_kv, keep))
+        dst = KvCache(k_out, v_out, lens_out, cache.h, cache.desc.scale)
+        assert dst.kq == cache.kq and dst.kv == cache.kv
+        if idx is None:
+            self.reserve(cache.B * cache.h_kv * max(keep, 0) * 4)
+        self._check(self.lib.ecospa_cache_evict(self.h, cache._ref, weights.data_ptr(), keep, recent, dst._ref, lens_out.data_ptr(),
+                                                _ptr(weights_out), _ptr(idx)), "ecospa_cache_evict")
+
+    def ecospa_logits_process(self, logits: torch.Tensor, out: Optional[torch.Tensor] = None, history: Optional[torch.Tensor] = None,
+                              history_len: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                              frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                              temperature: Optional[torch.Tensor] = None, bias_ids: Optional[torch.Tensor] = None,
+                              bias: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                              mask_row: Optional[torch.Tensor] = None, pick: Optional[torch.Tensor] = None,
+                              lse: Optional[torch.Tensor] = None):
+        """Penalties for the tokens of history [B, H] (int32), biases (ids and values [B, n]), temperature and masks (words [n_masks,
+        ceil(V / 32)], int32; mask_row int32 [B], -1: none) on logits [B, V] -> (pick int32 [B], lse float32 [B]); the processed logits go
+        to `out` (may be logits itself; None: not wanted).  Parameters: float32 [B]."""
+        Bsz, V = logits.shape
+        assert logits.stride(1) == 1 and (out is None or (out.shape == logits.shape and out.stride(1) == 1))
+        f32, i32 = torch.float32, torch.int32
+        assert all(t is None or (t.dtype == f32 and t.is_contiguous() and t.numel() == Bsz) for t in (repetition, frequency, presence, temperature, lse))
+        assert all(t is None or (t.dtype == i32 and t.is_contiguous() and t.numel() == Bsz) for t in (history_len, mask_row, pick))
+        assert history is None or (history.dtype == i32 and history.is_contiguous() and history.shape[0] == Bsz)
+        n_bias = 0 if bias is None else bias.shape[1]
+        assert n_bias == 0 or (bias.dtype == f32 and bias_ids.dtype == i32 and bias.is_contiguous() and bias_ids.is_contiguous()
+                               and bias.shape == bias_ids.shape == (Bsz, n_bias))
+        assert mask is None or (mask.dtype == i32 and mask.stride(1) == 1 and mask_row is not None)
+        pick = torch.empty(Bsz, dtype=i32, device=logits.device) if pick is None else pick
+        lse = torch.empty(Bsz, dtype=f32, device=logits.device) if lse is None else lse
+        self.reserve(self.lib.ecospa_logits_workspace_bytes(Bsz, V))
+        a = Logits(Bsz, V, dtype_code(logits.dtype), 0 if out is None else dtype_code(out.dtype), logits.data_ptr(), _ptr(out), logits.stride(0),
+                   0 if out is None else out.stride(0), _ptr(history), _ptr(history_len), 0 if history is None else history.shape[1], n_bias,
+                   _ptr(repetition), _ptr(frequency), _ptr(presence), _ptr(temperature), _ptr(bias_ids) if n_bias else None,
+                   _ptr(bias) if n_bias else None, _ptr(mask), _ptr(mask_row), 0 if mask is None else mask.stride(0),
+                   0 if mask is None else mask.shape[0], pick.data_ptr(), lse.data_ptr())
+        self._check(self.lib.ecospa_logits_process(self.h, C.byref(a)), "ecospa_logits_process")
+        return pick, lse
 
     # ---- parameter update ----------------------------------------------------------------------
     @staticmethod

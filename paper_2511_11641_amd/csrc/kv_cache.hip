@@ -1,0 +1,180 @@
+// Own caches of compact heads: new tokens in (rotated at each request's own position), evicted tokens out (kept rows gathered by the
+// accumulated attention weight).  Both move rows of at most 256 bytes and compute next to nothing: bound by memory traffic, or by
+// latency alone for the few rows of a decoding step.
+#include "common.h"
+
+#include "select_dev.h"
+
+int ecospa_cache_check(const ecospa_cache* c);      // prefix_attn.hip
+
+typedef float kv_floatx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 kv_bf16x8 __attribute__((ext_vector_type(8)));
+
+// ---------------------------------------------------------------------------------------------
+// Append: a thread takes 16 bytes of a row of the projection - eight dims of a query, key or value head of one token - turns the four
+// pairs in fp32 ((x0, x1) -> (x0 c - x1 s, x0 s + x1 c), rounded once) and writes them to their place.
+// ---------------------------------------------------------------------------------------------
+struct AppendArgs {
+  const bf16_t* qkv;
+  bf16_t *q, *k, *v;
+  float* weights;
+  const float *cos, *sin;
+  const int *lens, *pos;
+  long long ld_qkv, ld_q, k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  int T, L, L_tab, cap, h, h_kv, g, kq, kv;
+  int first_chunk, chunks;      // of a token's row: chunks in front of the first one that is moved (queries that stay where they are), chunks moved
+};
+__global__ __launch_bounds__(256) void cache_append_kernel(const AppendArgs a) {
+  const long long id = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+  const int token = static_cast<int>(id / a.chunks);
+  if (token >= a.T) return;
+  const int ch = a.first_chunk + static_cast<int>(id - static_cast<long long>(token) * a.chunks);
+  const uint4 x = *reinterpret_cast<const uint4*>(a.qkv + token * a.ld_qkv + ch * 8);
+  const int b = token / a.L, t = token - b * a.L, slot = a.lens[b] - a.L + t, at = a.cos ? a.pos[b] + t : 0;
+  const bool in = slot >= 0 && slot < a.cap && (!a.cos || (at >= 0 && at < a.L_tab));
+  const int cq = a.kq >> 3, nq = a.h * cq, nk = a.h_kv * cq, cv = a.kv >> 3;
+  if (ch >= nq + nk) {
+    const int head = (ch - nq - nk) / cv, d = (ch - nq - nk - head * cv) * 8;
+    if (in) *reinterpret_cast<uint4*>(a.v + b * a.v_sb + head * a.v_sh + slot * a.v_st + d) = x;
+    return;
+  }
+  const bool key = ch >= nq;
+  const int head = (key ? ch - nq : ch) / cq, d = ((key ? ch - nq : ch) - head * cq) * 8, kh = key ? head : head / a.g;
+  uint4 y = x;
+  if (a.cos && in) {
+    const long long tab = (static_cast<long long>(kh) * a.L_tab + at) * (a.kq >> 1) + (d >> 1);
+    const float4 c4 = *reinterpret_cast<const float4*>(a.cos + tab), s4 = *reinterpret_cast<const float4*>(a.sin + tab);
+    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    kv_floatx8 f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x0 = __uint_as_float(w[i] << 16), x1 = __uint_as_float(w[i] & 0xffff0000u);
+      f[2 * i] = x0 * c[i] - x1 * s[i];
+      f[2 * i + 1] = x0 * s[i] + x1 * c[i];
+    }
+    y = __builtin_bit_cast(uint4, __builtin_convertvector(f, kv_bf16x8));
+  }
+  if (!key) {
+    *reinterpret_cast<uint4*>(a.q + token * a.ld_q + ch * 8) = in ? y : uint4{0u, 0u, 0u, 0u};
+  } else if (in) {
+    *reinterpret_cast<uint4*>(a.k + b * a.k_sb + head * a.k_sh + slot * a.k_st + d) = y;
+    if (a.weights && d == 0) a.weights[(static_cast<long long>(b) * a.h_kv + head) * a.cap + slot] = 0.f;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Evict.  First launch: a workgroup per (request, key/value head) lists the rows that stay, ascending - the top of the weights of all but the
+// last `recent` rows by the radix selection of step 2, then those rows.  Second launch: the gather, 16 bytes a thread.
+// ---------------------------------------------------------------------------------------------
+struct EvictArgs {
+  const bf16_t *k, *v;
+  bf16_t *k_out, *v_out;
+  const float* weights;
+  float* weights_out;
+  const int* lens;
+  int *lens_out, *idx;
+  long long k_sb, k_sh, k_st, v_sb, v_sh, v_st, ko_sb, ko_sh, ko_st, vo_sb, vo_sh, vo_st;
+  int B, h_kv, cap, cap_out, own_max, keep, recent, kq, kv;
+};
+__device__ __forceinline__ int evict_len(const EvictArgs& a, int b) { return min(max(a.lens[b], 0), a.own_max); }
+__global__ __launch_bounds__(SELECT_THREADS) void cache_choose_kernel(const EvictArgs a) {
+  __shared__ SelectShared sh;
+  const int bh = blockIdx.x, b = bh / a.h_kv, n = evict_len(a, b);
+  int* const idx = a.idx + static_cast<long long>(bh) * a.keep;
+  if (threadIdx.x == 0 && bh == b * a.h_kv) a.lens_out[b] = min(n, a.keep);
+  if (n <= a.keep) {
+    for (int i = threadIdx.x; i < a.keep; i += SELECT_THREADS) idx[i] = i < n ? i : -1;
+    return;
+  }
+  const int old = n - a.recent, top = a.keep - a.recent;
+  for (int i = threadIdx.x; i < a.recent; i += SELECT_THREADS) idx[top + i] = old + i;
+  if (top == 0) return;
+  SelectItemDev t{};
+  t.scores = a.weights + static_cast<long long>(bh) * a.cap;
+  t.idx = idx;
+  t.n = old;
+  t.k = top;
+  t.groups = 1;
+  select_item_block(t, 0, sh);
+}
+__global__ __launch_bounds__(256) void cache_gather_kernel(const EvictArgs a) {
+  const int bh = blockIdx.y, b = bh / a.h_kv, hk = bh - b * a.h_kv, n = min(evict_len(a, b), a.keep);
+  const int cq = a.kq >> 3, per = cq + (a.kv >> 3);
+  const int id = blockIdx.x * 256 + threadIdx.x, i = id / per, c = id - i * per;
+  if (i >= n) return;
+  const int j = a.idx[static_cast<long long>(bh) * a.keep + i];
+  if (c < cq)
+    *reinterpret_cast<uint4*>(a.k_out + b * a.ko_sb + hk * a.ko_sh + i * a.ko_st + c * 8) = *reinterpret_cast<const uint4*>(a.k + b * a.k_sb + hk * a.k_sh + j * a.k_st + c * 8);
+  else
+    *reinterpret_cast<uint4*>(a.v_out + b * a.vo_sb + hk * a.vo_sh + i * a.vo_st + (c - cq) * 8) =
+        *reinterpret_cast<const uint4*>(a.v + b * a.v_sb + hk * a.v_sh + j * a.v_st + (c - cq) * 8);
+  if (c == 0 && a.weights_out) a.weights_out[static_cast<long long>(bh) * a.cap_out + i] = a.weights[static_cast<long long>(bh) * a.cap + j];
+}
+
+// ---------------------------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------------------------
+extern "C" int ecospa_cache_append(ecospa_ctx* ctx, const ecospa_cache* c, int L, const void* qkv, long long ld_qkv, const int* pos,
+                                   const float* rope_cos, const float* rope_sin, int L_tab, void* q, long long ld_q, float* weights) {
+  if (!ctx || !qkv || !rope_cos != !rope_sin || (rope_cos && (!pos || !q))) return ECOSPA_ERR_NULL;
+  const int rc = ecospa_cache_check(c);
+  if (rc != ECOSPA_OK) return rc;
+  const int nq = c->h * c->kp_qk, nk = c->h_kv * c->kp_qk, nv = c->h_kv * c->kp_vo;
+  if (L < 1 || static_cast<long long>(c->B) * L * c->h > (1ll << 30) || static_cast<long long>(c->B) * c->h_kv > 65535) return ECOSPA_ERR_SHAPE;
+  if (ld_qkv < nq + nk + nv || (q && ld_q < nq) || (rope_cos && L_tab < 1)) return ECOSPA_ERR_SHAPE;
+  if (!aligned16(qkv) || ld_qkv % 8 || (q && (!aligned16(q) || ld_q % 8)) || !aligned16(rope_cos) || !aligned16(rope_sin)) return ECOSPA_ERR_ALIGN;
+  AppendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.qkv = static_cast<const bf16_t*>(qkv); a.q = static_cast<bf16_t*>(q); a.k = static_cast<bf16_t*>(c->k); a.v = static_cast<bf16_t*>(c->v);
+  a.weights = weights; a.cos = rope_cos; a.sin = rope_sin; a.lens = c->lens; a.pos = pos;
+  a.ld_qkv = ld_qkv; a.ld_q = ld_q; a.k_sb = c->k_sb; a.k_sh = c->k_sh; a.k_st = c->k_st; a.v_sb = c->v_sb; a.v_sh = c->v_sh; a.v_st = c->v_st;
+  a.T = c->B * L; a.L = L; a.L_tab = L_tab; a.cap = c->cap; a.h = c->h; a.h_kv = c->h_kv; a.g = c->h / c->h_kv; a.kq = c->kp_qk; a.kv = c->kp_vo;
+  a.first_chunk = q ? 0 : nq / 8;
+  a.chunks = (nq + nk + nv) / 8 - a.first_chunk;
+  const long long n = static_cast<long long>(a.T) * a.chunks;
+  hipLaunchKernelGGL(cache_append_kernel, dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, ctx->stream, a);
+  ECOSPA_CHECK_LAUNCH(ctx, "cache_append_kernel");
+  return ECOSPA_OK;
+}
+
+extern "C" int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src, const float* weights, int keep, int recent, const ecospa_cache* dst,
+                                  int* lens_out, float* weights_out, int* idx) {
+  if (!ctx || !src || !dst || !weights || !lens_out || !dst->k || !dst->v) return ECOSPA_ERR_NULL;
+  int rc = ecospa_cache_check(src);
+  if (rc != ECOSPA_OK) return rc;
+  ecospa_cache d = *dst;      // its lengths are an output, its prefix and bound play no part
+  d.lens = lens_out;
+  d.P = 0;
+  d.own_max = 0;
+  d.scale = src->scale;
+  rc = ecospa_cache_check(&d);
+  if (rc != ECOSPA_OK) return rc;
+  if (d.B != src->B || d.h_kv != src->h_kv || d.kp_qk != src->kp_qk || d.kp_vo != src->kp_vo || static_cast<long long>(src->B) * src->h_kv > 65535)
+    return ECOSPA_ERR_SHAPE;
+  if (keep < 1 || recent < 0 || recent > keep || d.cap < keep) return ECOSPA_ERR_K;
+  EvictArgs a;
+  memset(&a, 0, sizeof(a));
+  if (!idx) {
+    WsCarver ws(ctx->ws, ctx->ws_bytes);
+    idx = static_cast<int*>(ws.take(static_cast<size_t>(src->B) * src->h_kv * keep * sizeof(int)));
+    if (!ws.ok()) return ECOSPA_ERR_WORKSPACE;
+  }
+  a.k = static_cast<const bf16_t*>(src->k); a.v = static_cast<const bf16_t*>(src->v);
+  a.k_out = static_cast<bf16_t*>(d.k); a.v_out = static_cast<bf16_t*>(d.v);
+  a.weights = weights; a.weights_out = weights_out; a.lens = src->lens; a.lens_out = lens_out; a.idx = idx;
+  a.k_sb = src->k_sb; a.k_sh = src->k_sh; a.k_st = src->k_st; a.v_sb = src->v_sb; a.v_sh = src->v_sh; a.v_st = src->v_st;
+  a.ko_sb = d.k_sb; a.ko_sh = d.k_sh; a.ko_st = d.k_st; a.vo_sb = d.v_sb; a.vo_sh = d.v_sh; a.vo_st = d.v_st;
+  a.B = src->B; a.h_kv = src->h_kv; a.cap = src->cap; a.cap_out = d.cap; a.own_max = src->own_max; a.keep = keep; a.recent = recent;
+  a.kq = src->kp_qk; a.kv = src->kp_vo;
+  const int groups = a.B * a.h_kv;
+  hipLaunchKernelGGL(cache_choose_kernel, dim3(groups), dim3(SELECT_THREADS), 0, ctx->stream, a);
+  ECOSPA_CHECK_LAUNCH(ctx, "cache_choose_kernel");
+  const long long n = static_cast<long long>(keep < a.own_max ? keep : a.own_max) * ((a.kq + a.kv) / 8);
+  if (n > 0x7fffffffll - 256) return ECOSPA_ERR_SHAPE;
+  if (n > 0) {
+    hipLaunchKernelGGL(cache_gather_kernel, dim3(static_cast<unsigned>((n + 255) / 256), groups), dim3(256), 0, ctx->stream, a);
+    ECOSPA_CHECK_LAUNCH(ctx, "cache_gather_kernel");
+  }
+  return ECOSPA_OK;
+}
