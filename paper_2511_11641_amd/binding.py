@@ -248,6 +248,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _dense(t: Optional[torch.Tensor], dtype: torch.dtype, n: int) -> Optional[int]:
+    """Address of a contiguous tensor of n elements of this type (None: no tensor)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous {dtype} tensor of {n} elements, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
 def round_up(x: int, m: int) -> int:
     return (x + m - 1) // m * m
 
@@ -262,20 +271,21 @@ class KvCache:
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, h: int, scale: float, pk: Optional[torch.Tensor] = None,
                  pv: Optional[torch.Tensor] = None, own_max: Optional[int] = None):
-        Bsz, h_kv, cap, kq = k.shape
-        assert v.shape[:3] == k.shape[:3] and v.dtype == k.dtype and k.stride(3) == 1 and v.stride(3) == 1
-        assert lens.dtype == torch.int32 and lens.is_contiguous() and lens.numel() == Bsz and (pk is None) == (pv is None)
+        (Bsz, h_kv, cap, kq), (k_sb, k_sh, k_st, k_unit) = k.shape, k.stride()
+        (vB, vh, vcap, kv), (v_sb, v_sh, v_st, v_unit) = v.shape, v.stride()
+        assert (vB, vh, vcap) == (Bsz, h_kv, cap) and v.dtype == k.dtype and k_unit == 1 and v_unit == 1 and (pk is None) == (pv is None)
         self.k, self.v, self.lens, self.pk, self.pv = k, v, lens, pk, pv
-        self.B, self.h, self.h_kv, self.cap, self.kq, self.kv = Bsz, h, h_kv, cap, kq, v.shape[3]
-        P, prefix = 0, (0, 0, 0, 0)
+        self.B, self.h, self.h_kv, self.cap, self.kq, self.kv, self.scale = Bsz, h, h_kv, cap, kq, kv, scale
+        self.nq, self.no, self.nqkv, self.n_weights = h * kq, h * kv, (h + h_kv) * kq + h_kv * kv, Bsz * h_kv * cap
+        P, prefix = 0, (None, None, 0, 0, 0, 0)
         if pk is not None:
             P = pk.shape[1]
-            assert pk.shape == (h_kv, P, kq) and pv.shape == (h_kv, P, self.kv) and pk.dtype == k.dtype and pv.dtype == k.dtype
+            assert pk.shape == (h_kv, P, kq) and pv.shape == (h_kv, P, kv) and pk.dtype == k.dtype and pv.dtype == k.dtype
             assert pk.stride(2) == 1 and pv.stride(2) == 1
-            prefix = (pk.stride(0), pk.stride(1), pv.stride(0), pv.stride(1))
-        self.desc = Cache(dtype_code(k.dtype), Bsz, h, h_kv, kq, self.kv, cap, cap if own_max is None else own_max, P, scale, k.data_ptr(),
-                          v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), v.stride(0), v.stride(1), v.stride(2),
-                          _ptr(pk) if P else None, _ptr(pv) if P else None, *prefix, lens.data_ptr())
+            if P:
+                prefix = (pk.data_ptr(), pv.data_ptr(), pk.stride(0), pk.stride(1), pv.stride(0), pv.stride(1))
+        self.desc = Cache(dtype_code(k.dtype), Bsz, h, h_kv, kq, kv, cap, cap if own_max is None else own_max, P, scale, k.data_ptr(), v.data_ptr(),
+                          k_sb, k_sh, k_st, v_sb, v_sh, v_st, *prefix, _dense(lens, torch.int32, Bsz))
         self._ref = C.byref(self.desc)
         self._need = {}
 
@@ -308,6 +318,7 @@ class Context:
             raise EcospaError(rc, "ecospa_create")
         self.h = h
         self._ws: Optional[torch.Tensor] = None
+        self._logits_need: dict = {}      # workspace of a (B, V)
 
     def __del__(self):
         try:
@@ -666,57 +677,61 @@ class Context:
         return loss
 
     # ---- serving -------------------------------------------------------------------------------
-    def _tokens(self, cache: KvCache, x: torch.Tensor) -> int:
-        assert x.dim() == 2 and x.stride(1) == 1 and x.dtype == torch.bfloat16 and x.shape[0] % cache.B == 0
-        return x.shape[0] // cache.B
-
-    def _weights_ok(self, cache: KvCache, w: Optional[torch.Tensor], cap: int) -> bool:
-        return w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.shape == (cache.B, cache.h_kv, cap))
+    @staticmethod
+    def _rows(x: torch.Tensor, width: int):
+        """(rows, leading dimension) of a bf16 matrix of at least `width` columns."""
+        (T, w), (ld, unit) = x.shape, x.stride()
+        if w < width or unit != 1 or x.dtype != torch.bfloat16:
+            raise ValueError(f"expected bf16 rows of {width} elements, got {x.dtype} {tuple(x.shape)}")
+        return T, ld
 
     def ecospa_cache_append(self, cache: KvCache, qkv: torch.Tensor, pos: Optional[torch.Tensor] = None, rope=None,
                             q: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None):
         """The L = rows / B new tokens of every request (rows of the projection: Q | K | V columns) become the last L rows of its cache;
         cache.lens counts them already.  rope: (cos, sin) [h_kv, L_tab, kp_qk / 2] turns queries (into q) and keys by the angles of
         positions pos[b] + t; weights [B, h_kv, cap]: the new rows' accumulated weights are set to zero."""
-        L = self._tokens(cache, qkv)
-        assert qkv.shape[1] >= (cache.h + cache.h_kv) * cache.kq + cache.h_kv * cache.kv
-        assert q is None or (self._tokens(cache, q) == L and q.shape[1] >= cache.h * cache.kq)
-        assert pos is None or (pos.dtype == torch.int32 and pos.is_contiguous() and pos.numel() == cache.B)
-        assert self._weights_ok(cache, weights, cache.cap)
-        cos, sin = rope if rope is not None else (None, None)
-        if cos is not None:
-            assert cos.shape == sin.shape and cos.dtype == sin.dtype == torch.float32 and cos.is_contiguous() and sin.is_contiguous()
-            assert cos.shape[0] == cache.h_kv and cos.shape[2] == cache.kq // 2
-        self._check(self.lib.ecospa_cache_append(self.h, cache._ref, L, qkv.data_ptr(), qkv.stride(0), _ptr(pos), _ptr(cos), _ptr(sin),
-                                                 0 if cos is None else cos.shape[1], _ptr(q), 0 if q is None else q.stride(0),
-                                                 _ptr(weights)), "ecospa_cache_append")
+        T, ld = self._rows(qkv, cache.nqkv)
+        Tq, ldq = (T, 0) if q is None else self._rows(q, cache.nq)
+        if T % cache.B or Tq != T:
+            raise ValueError(f"{T} rows (queries {Tq}) for {cache.B} requests")
+        cos_ptr = sin_ptr = None
+        tab = 0
+        if rope is not None:
+            cos, sin = rope
+            tab = cos.shape[1]
+            n = cache.h_kv * tab * (cache.kq // 2)
+            cos_ptr, sin_ptr = _dense(cos, torch.float32, n), _dense(sin, torch.float32, n)
+        self._check(self.lib.ecospa_cache_append(self.h, cache._ref, T // cache.B, qkv.data_ptr(), ld, _dense(pos, torch.int32, cache.B), cos_ptr,
+                                                 sin_ptr, tab, _ptr(q), ldq, _dense(weights, torch.float32, cache.n_weights)), "ecospa_cache_append")
 
     def ecospa_prefix_attn(self, cache: KvCache, q: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None,
                            weights: Optional[torch.Tensor] = None, weights_out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """o [B*L, h * kp_vo] = attention of the new tokens' queries q [B*L, h * kp_qk] over the shared prefix and the own caches; lse
         float32 [B, h, L]; weights_out [B, h_kv, cap] = weights (None: zeros) + what every own key received."""
-        L = self._tokens(cache, q)
-        assert self._tokens(cache, o) == L and q.shape[1] >= cache.h * cache.kq and o.shape[1] >= cache.h * cache.kv
-        assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == cache.B * cache.h * L)
-        assert self._weights_ok(cache, weights, cache.cap) and self._weights_ok(cache, weights_out, cache.cap)
+        T, ldq = self._rows(q, cache.nq)
+        To, ldo = self._rows(o, cache.no)
+        L = T // cache.B
+        if T % cache.B or To != T:
+            raise ValueError(f"{T} rows (outputs {To}) for {cache.B} requests")
         self.reserve(cache.workspace_bytes(L))
-        self._check(self.lib.ecospa_prefix_attn(self.h, cache._ref, L, q.data_ptr(), q.stride(0), o.data_ptr(), o.stride(0), _ptr(lse),
-                                                _ptr(weights), _ptr(weights_out)), "ecospa_prefix_attn")
+        f32 = torch.float32
+        self._check(self.lib.ecospa_prefix_attn(self.h, cache._ref, L, q.data_ptr(), ldq, o.data_ptr(), ldo, _dense(lse, f32, T * cache.h),
+                                                _dense(weights, f32, cache.n_weights), _dense(weights_out, f32, cache.n_weights)), "ecospa_prefix_attn")
         return o
 
     def ecospa_cache_evict(self, cache: KvCache, weights: torch.Tensor, keep: int, recent: int, k_out: torch.Tensor, v_out: torch.Tensor,
                            lens_out: torch.Tensor, weights_out: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None):
         """The last `recent` rows of every cache and, of the others, those with the largest weights, `keep` in all, gathered in order into
         k_out, v_out [B, h_kv, cap_out, kp]; lens_out int32 [B]; weights_out float32 [B, h_kv, cap_out]; idx int32 [B, h_kv, keep]."""
-        assert k_out.shape[:2] == (cache.B, cache.h_kv) and self._weights_ok(cache, weights, cache.cap)
-        assert self._weights_ok(cache, weights_out, k_out.shape[2]) and lens_out.data_ptr() != cache.lens.data_ptr()
-        assert idx is None or (idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape == (cache.B, cache.h_kv, keep))
-        dst = KvCache(k_out, v_out, lens_out, cache.h, cache.desc.scale)
-        assert dst.kq == cache.kq and dst.kv == cache.kv
+        dst = KvCache(k_out, v_out, lens_out, cache.h, cache.scale)
+        if (dst.B, dst.h_kv, dst.kq, dst.kv) != (cache.B, cache.h_kv, cache.kq, cache.kv) or lens_out.data_ptr() == cache.lens.data_ptr():
+            raise ValueError("the new cache differs in requests, heads or widths, or shares its lengths with the old one")
         if idx is None:
             self.reserve(cache.B * cache.h_kv * max(keep, 0) * 4)
-        self._check(self.lib.ecospa_cache_evict(self.h, cache._ref, weights.data_ptr(), keep, recent, dst._ref, lens_out.data_ptr(),
-                                                _ptr(weights_out), _ptr(idx)), "ecospa_cache_evict")
+        f32 = torch.float32
+        self._check(self.lib.ecospa_cache_evict(self.h, cache._ref, _dense(weights, f32, cache.n_weights), keep, recent, dst._ref, dst.desc.lens,
+                                                _dense(weights_out, f32, dst.n_weights), _dense(idx, torch.int32, cache.B * cache.h_kv * keep)),
+                    "ecospa_cache_evict")
 
     def ecospa_logits_process(self, logits: torch.Tensor, out: Optional[torch.Tensor] = None, history: Optional[torch.Tensor] = None,
                               history_len: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
@@ -728,24 +743,32 @@ class Context:
         """Penalties for the tokens of history [B, H] (int32), biases (ids and values [B, n]), temperature and masks (words [n_masks,
         ceil(V / 32)], int32; mask_row int32 [B], -1: none) on logits [B, V] -> (pick int32 [B], lse float32 [B]); the processed logits go
         to `out` (may be logits itself; None: not wanted).  Parameters: float32 [B]."""
-        Bsz, V = logits.shape
-        assert logits.stride(1) == 1 and (out is None or (out.shape == logits.shape and out.stride(1) == 1))
+        (Bsz, V), (ld, unit) = logits.shape, logits.stride()
         f32, i32 = torch.float32, torch.int32
-        assert all(t is None or (t.dtype == f32 and t.is_contiguous() and t.numel() == Bsz) for t in (repetition, frequency, presence, temperature, lse))
-        assert all(t is None or (t.dtype == i32 and t.is_contiguous() and t.numel() == Bsz) for t in (history_len, mask_row, pick))
-        assert history is None or (history.dtype == i32 and history.is_contiguous() and history.shape[0] == Bsz)
-        n_bias = 0 if bias is None else bias.shape[1]
-        assert n_bias == 0 or (bias.dtype == f32 and bias_ids.dtype == i32 and bias.is_contiguous() and bias_ids.is_contiguous()
-                               and bias.shape == bias_ids.shape == (Bsz, n_bias))
-        assert mask is None or (mask.dtype == i32 and mask.stride(1) == 1 and mask_row is not None)
+        ld_out = out_dtype = n_bias = H = n_masks = ld_mask = 0
+        bias_ptr = ids_ptr = mask_ptr = hist_ptr = out_ptr = None
+        assert unit == 1
+        if out is not None:
+            (ld_out, unit), out_dtype, out_ptr = out.stride(), dtype_code(out.dtype), out.data_ptr()
+            assert unit == 1 and out.shape == logits.shape
+        if history is not None:
+            H = history.shape[1]
+            hist_ptr = _dense(history, i32, Bsz * H)
+        if bias is not None:
+            n_bias = bias.shape[1]
+            bias_ptr, ids_ptr = _dense(bias, f32, Bsz * n_bias), _dense(bias_ids, i32, Bsz * n_bias)
+        if mask is not None:
+            (ld_mask, unit), n_masks, mask_ptr = mask.stride(), mask.shape[0], mask.data_ptr()
+            assert unit == 1 and mask.dtype == i32 and mask_row is not None
         pick = torch.empty(Bsz, dtype=i32, device=logits.device) if pick is None else pick
         lse = torch.empty(Bsz, dtype=f32, device=logits.device) if lse is None else lse
-        self.reserve(self.lib.ecospa_logits_workspace_bytes(Bsz, V))
-        a = Logits(Bsz, V, dtype_code(logits.dtype), 0 if out is None else dtype_code(out.dtype), logits.data_ptr(), _ptr(out), logits.stride(0),
-                   0 if out is None else out.stride(0), _ptr(history), _ptr(history_len), 0 if history is None else history.shape[1], n_bias,
-                   _ptr(repetition), _ptr(frequency), _ptr(presence), _ptr(temperature), _ptr(bias_ids) if n_bias else None,
-                   _ptr(bias) if n_bias else None, _ptr(mask), _ptr(mask_row), 0 if mask is None else mask.stride(0),
-                   0 if mask is None else mask.shape[0], pick.data_ptr(), lse.data_ptr())
+        need = self._logits_need.get((Bsz, V))
+        if need is None:
+            need = self._logits_need[Bsz, V] = self.lib.ecospa_logits_workspace_bytes(Bsz, V)
+        self.reserve(need)
+        a = Logits(Bsz, V, dtype_code(logits.dtype), out_dtype, logits.data_ptr(), out_ptr, ld, ld_out, hist_ptr, _dense(history_len, i32, Bsz), H,
+                   n_bias, _dense(repetition, f32, Bsz), _dense(frequency, f32, Bsz), _dense(presence, f32, Bsz), _dense(temperature, f32, Bsz),
+                   ids_ptr, bias_ptr, mask_ptr, _dense(mask_row, i32, Bsz), ld_mask, n_masks, _dense(pick, i32, Bsz), _dense(lse, f32, Bsz))
         self._check(self.lib.ecospa_logits_process(self.h, C.byref(a)), "ecospa_logits_process")
         return pick, lse
 
