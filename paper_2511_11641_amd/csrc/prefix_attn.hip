@@ -412,22 +412,25 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
 // Which rows an item has: ROWS_16, ROWS_32: up to 16 or 32, its key tiles shared out over the wavefronts; ROWS_128: 32 a wavefront.
 enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_128 = 2 };
 // KIND: rows of every item; prefix items have ROWS_128 where PREFIX_128 says so.
+// Two wavefronts a SIMD at least: the register file then has no accumulation half, and the scores need no moves between the halves.
 template <int DQ, int DV, int KIND, bool PREFIX_128>
-__global__ __launch_bounds__(256) void prefix_attn_kernel(const PrefixArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_attn_kernel(const PrefixArgs a) {
   extern __shared__ __attribute__((aligned(16))) bf16_t lds_all[];      // one object: see attn.hip
   if (PREFIX_128 && static_cast<int>(blockIdx.x) < a.p_items) prefix_rows<DQ, DV, 2, true>(a, lds_all);
   else prefix_rows<DQ, DV, KIND == ROWS_16 ? 1 : 2, KIND == ROWS_128>(a, lds_all);
 }
 
 // ---------------------------------------------------------------------------------------------
-// Join: a wavefront puts the pieces of a row together.  Lanes are (piece, four dims); the maximum over the pieces comes first, then the
-// weighted sums, added over the lanes of equal dims in a fixed order.
+// Join: a workgroup puts the pieces of a row together.  Threads are (piece, four dims); a thread weighs its pieces against the maximum of its
+// own, four of them asked for at a time (what counts is how many latencies follow on each other), then the threads of equal dims are added up
+// against the row's maximum in a fixed order.
 // ---------------------------------------------------------------------------------------------
-template <int W>      // lanes of a piece: kp_vo / 4 rounded up to a power of two
+template <int W>      // threads of a piece: kp_vo / 4 rounded up to a power of two
 __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, int kt, int row_tile) {
-  const int lane = threadIdx.x & 63;
-  const long long at = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (at >= static_cast<long long>(a.h_kv) * a.rows) return;
+  constexpr int GROUPS = 256 / W;
+  __shared__ floatx4 so[GROUPS][W];
+  __shared__ float sm[GROUPS], sl[GROUPS];
+  const long long at = blockIdx.x;
   const int hk = static_cast<int>(at / a.rows), row = static_cast<int>(at - static_cast<long long>(hk) * a.rows);
   const int token = row / a.g, b = token / a.L, head = hk * a.g + (row - token * a.g);
   // own pieces: as prefix_item() cuts them for the tile of rows that this row is in
@@ -435,30 +438,58 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
   const int own_n = own_visible(own_len(a, b), a.L, (min(tile0 + row_tile, a.own_rows) - 1) / a.g);
   const int own_tiles = (own_n + kt - 1) / kt + (a.joint ? a.p_tiles : 0);
   const int n = (a.joint ? 0 : a.p_chunks) + (own_tiles + a.o_chunk - 1) / a.o_chunk;
-  const float* const ml = a.part_ml + 2 * at * a.slots;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, ml[2 * i]);
-  m = wave_max(m);
-  const int piece = lane / W, d = (lane % W) * 4;
-  float l = 0.f;
+  const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + at * a.slots;
+  const int grp = threadIdx.x / W, lane = threadIdx.x % W, d = min(lane * 4, a.kv - 4);
+  const float* const po = a.part_o + at * a.slots * a.kv + d;
+  float m = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = piece; i < n; i += 64 / W) {
-    const float2 x = *reinterpret_cast<const float2*>(ml + 2 * i);
-    const float w = x.x == m ? (m == -INFINITY ? 0.f : 1.f) : __builtin_amdgcn_exp2f(x.x - m);
-    l += w * x.y;
-    if (d < a.kv) {
-      const floatx4 p = *reinterpret_cast<const floatx4*>(a.part_o + (at * a.slots + i) * a.kv + d);
+  for (int i0 = grp; i0 < n; i0 += 4 * GROUPS) {
+    float2 x[4];
+    floatx4 p[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += w * p[e];
+    for (int j = 0; j < 4; ++j) {
+      const int i = min(i0 + j * GROUPS, n - 1);
+      x[j] = ml[i];
+      p[j] = *reinterpret_cast<const floatx4*>(po + static_cast<long long>(i) * a.kv);
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * GROUPS >= n) x[j].x = -INFINITY;
+      top = fmaxf(top, x[j].x);
+    }
+    const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(m - ref);
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w = x[j].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[j].x - ref);
+      l += w * x[j].y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += w * p[j][e];
     }
   }
+  so[grp][lane] = o;
+  if (lane == 0) { sm[grp] = m; sl[grp] = l; }
+  __syncthreads();
+  if (grp > 0) return;
+  m = sm[0];
 #pragma unroll
-  for (int s = W; s < 64; s <<= 1) {
-    l += __shfl_xor(l, s, 64);
+  for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, sm[i]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s, 64);
+  for (int i = 0; i < GROUPS; ++i) {
+    const float w = __builtin_amdgcn_exp2f(sm[i] - ref);
+    const floatx4 p = so[i][lane];
+    l += w * sl[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += w * p[e];
   }
-  if (piece == 0 && d < a.kv) {
+  if (lane * 4 < a.kv) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] *= inv;
@@ -690,7 +721,7 @@ extern "C" int ecospa_prefix_attn(ecospa_ctx* ctx, const ecospa_cache* cache, in
   if (e != hipSuccess) return hip_fail(ctx, e, "prefix_attn_kernel");
   if (a.slots) {
     const long long rows = static_cast<long long>(a.h_kv) * a.rows;
-    const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
+    const dim3 grid(static_cast<unsigned>(rows));
     if (a.kv <= 32) hipLaunchKernelGGL(prefix_join_kernel<8>, grid, dim3(256), 0, ctx->stream, a, p.kt, p.join_row_tile);
     else if (a.kv <= 64) hipLaunchKernelGGL(prefix_join_kernel<16>, grid, dim3(256), 0, ctx->stream, a, p.kt, p.join_row_tile);
     else hipLaunchKernelGGL(prefix_join_kernel<32>, grid, dim3(256), 0, ctx->stream, a, p.kt, p.join_row_tile);
