@@ -541,8 +541,9 @@ int ecospa_cache_append(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int
  * itself; NULL: zeros) plus the probabilities that the queries of its group gave it: the accumulated attention weight that
  * ecospa_cache_evict goes by.  Entries beyond lens[b] are left as they are.
  * Keys a query does not see carry no weight, but the values of the request's other new tokens have to be finite numbers.
- * Workspace: ecospa_prefix_attn_workspace_bytes (host-only query; 0 when none is needed or on bad input). */
-size_t ecospa_prefix_attn_workspace_bytes(const ecospa_cache* cache /*host*/, int L);
+ * Workspace: ecospa_prefix_attn_workspace_bytes (host-only query, with_weights: weights_out is given; 0 when none is needed or on
+ * bad input). */
+size_t ecospa_prefix_attn_workspace_bytes(const ecospa_cache* cache /*host*/, int L, int with_weights);
 int ecospa_prefix_attn(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int L, const void* q, long long ld_q, void* o,
                        long long ld_o, float* lse, const float* weights_in, float* weights_out);
 

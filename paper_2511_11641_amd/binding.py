@@ -220,7 +220,7 @@ def load() -> C.CDLL:
     lib.ecospa_cache_append.restype = ci
     lib.ecospa_prefix_attn.argtypes = [vp, C.POINTER(Cache), ci, vp, ll, vp, ll, vp, vp, vp]
     lib.ecospa_prefix_attn.restype = ci
-    lib.ecospa_prefix_attn_workspace_bytes.argtypes = [C.POINTER(Cache), ci]
+    lib.ecospa_prefix_attn_workspace_bytes.argtypes = [C.POINTER(Cache), ci, ci]
     lib.ecospa_prefix_attn_workspace_bytes.restype = sz
     lib.ecospa_cache_evict.argtypes = [vp, C.POINTER(Cache), vp, ci, ci, C.POINTER(Cache), vp, vp, vp]
     lib.ecospa_cache_evict.restype = ci
@@ -297,10 +297,10 @@ class KvCache:
     def own_max(self, n: int):
         self.desc.own_max = n
 
-    def workspace_bytes(self, L: int) -> int:
-        key = (L, self.desc.own_max)
+    def workspace_bytes(self, L: int, weights: bool) -> int:
+        key = (L, weights, self.desc.own_max)
         if key not in self._need:
-            self._need[key] = load().ecospa_prefix_attn_workspace_bytes(self._ref, L)
+            self._need[key] = load().ecospa_prefix_attn_workspace_bytes(self._ref, L, int(weights))
         return self._need[key]
 
 
@@ -713,7 +713,7 @@ class Context:
         L = T // cache.B
         if T % cache.B or To != T:
             raise ValueError(f"{T} rows (outputs {To}) for {cache.B} requests")
-        self.reserve(cache.workspace_bytes(L))
+        self.reserve(cache.workspace_bytes(L, weights_out is not None))
         f32 = torch.float32
         self._check(self.lib.ecospa_prefix_attn(self.h, cache._ref, L, q.data_ptr(), ldq, o.data_ptr(), ldo, _dense(lse, f32, T * cache.h),
                                                 _dense(weights, f32, cache.n_weights), _dense(weights_out, f32, cache.n_weights)), "ecospa_prefix_attn")

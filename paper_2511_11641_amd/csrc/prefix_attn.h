@@ -1,0 +1,535 @@
+// Attention of a few new tokens of B requests over a prefix that all of them share and over caches of their own, on compact heads.
+//
+// With s_j = scale q.k_j over the P prefix keys and the own keys that the query sees, o = sum_j exp(s_j - lse) v_j, lse = log sum_j exp(s_j).
+// Both sums are carried over tiles of keys against a running maximum (m, l, O), and pieces of them over disjoint keys join exactly:
+// (m, l, O) + (m', l', O') = (M, l e^(m-M) + l' e^(m'-M), O e^(m-M) + O' e^(m'-M)).
+//
+// The prefix is the same for every request, so the rows of a key/value head - query heads of its group x new tokens x requests - are one
+// matrix and every prefix key is read once for all of them; the own caches are read once each for the rows of their request.  Work is cut
+// into items (rows x range of keys, prefix or own); items of the same rows leave (m, l, O) in the workspace and a second launch joins them.
+//
+// Layout: scores are computed transposed on v_mfma_f32_16x16x32_bf16, S^T = K Q^T (16 keys x 16 rows): a row of the softmax is a lane's
+// column, and the four result registers of two key tiles are, rounded to bf16, the B operand of O^T = V^T P^T without going through LDS.
+// The matching V^T operand comes from transposing LDS reads.  Columns of 16 rather than 32: most calls have few rows (a token of a request
+// is g = h / h_kv rows), and the exponentials of unused columns are the largest cost beside the memory.
+//
+// Rounding: scores, maxima, sums and accumulators are fp32; the probabilities enter the second product rounded to bf16 (the matrix
+// unit's type), the denominator is summed from the unrounded ones, so that lse and the weights keep fp32 accuracy.
+#pragma once
+#include "attn_tile.h"
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+struct PrefixArgs {
+  const bf16_t *q, *k, *v, *pk, *pv;
+  bf16_t* o;
+  float* lse;              // [B, h, L] or null
+  float *part_o, *part_ml;   // workspace: [h_kv][rows][slots][kp_vo] and [h_kv][rows][slots][2] (maximum in score * scale * log2 e, sum)
+  const int* lens;
+  long long ld_q, ld_o, k_sb, k_sh, k_st, v_sb, v_sh, v_st, pk_sh, pk_st, pv_sh, pv_st;
+  int B, L, h, h_kv, g, kq, kv, P, own_max;
+  float sc;                // scale * log2 e
+  int rows;                // B * L * g rows of a key/value head
+  int own_rows;            // L * g of them belong to a request
+  int joint;               // items run over the prefix and then the request's own keys; otherwise over one of them
+  int p_tiles;             // key tiles of the prefix, as the items that read it cut it
+  int p_chunks, p_chunk, p_row_tiles;      // prefix items: chunks, key tiles of a chunk, tiles of rows
+  int o_chunks, o_chunk, o_row_tiles;      // own (or joint) items
+  int p_items;             // prefix items in front of the others in the grid
+  int slots;               // pieces per row in the workspace; 0: every item is all of its rows
+  float* scores;           // workspace: [B][h_kv][own_rows][own_pad] scores of the own keys times scale * log2 e, null: not wanted
+  int own_pad;
+  const float* w_in;       // with scores: the weights before and after
+  float* w_out;
+  int cap;
+};
+
+// own keys of request b that its new token t sees (the new tokens are the last L rows of the cache)
+__device__ __forceinline__ int own_len(const PrefixArgs& a, int b) { return min(max(a.lens[b], 0), a.own_max); }
+__device__ __forceinline__ int own_visible(int n, int L, int t) { return min(max(n - L + 1 + t, 0), n); }
+
+// Direct global->LDS loads of [KT rows][D] tiles, by one wavefront (WAVES = 1) or shared out over the workgroup's four.  An instruction
+// fills 64 / (D / 8) consecutive rows; the swizzle of the LDS tile is applied on the global side.  Rows beyond `valid` repeat the last valid one
+// (nothing behind the end of a cache is read), dims beyond the kept width the last kept chunk: stand-ins that masks and zero operands keep out.
+template <int D, int KT, int WAVES>
+struct KvLoader {
+  static constexpr int CPR = D / 8, RPI = 64 / CPR, PER = (KT / RPI) / WAVES, NC = D == 32 ? 1 : (D == 64 ? 2 : 4);
+  static_assert(PER >= 1, "a tile is at least an instruction of every wavefront");
+  unsigned col[NC];      // byte offset of the lane's chunk, by the parity of the instruction (the swizzle repeats every 16 rows)
+  int row0, wave;
+  __device__ __forceinline__ void init(int kp) {
+    const int lane = threadIdx.x & 63;
+    wave = WAVES == 1 ? 0 : static_cast<int>(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    row0 = wave * (PER * RPI) + lane / CPR;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) col[i] = static_cast<unsigned>(min(((lane % CPR) ^ nat_swz<D>(row0 + i * RPI)) * 8, kp - 8) * 2);
+  }
+  __device__ __forceinline__ void issue(bf16_t* tile, const char* base, unsigned ldb, int valid) const {
+    lds_bf16_t* const dst = (lds_bf16_t*)tile + wave * (PER * 512);
+    if (valid >= KT) {
+      const unsigned at = static_cast<unsigned>(row0) * ldb;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        unsigned o = at + col[i % NC];
+        asm volatile("" : "+v"(o));      // keeps the offset a lane register at the load
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + static_cast<unsigned long long>(i * RPI) * ldb + o), dst + i * 512, 16, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        unsigned o = static_cast<unsigned>(min(row0 + i * RPI, valid - 1)) * ldb + col[i % NC];
+        asm volatile("" : "+v"(o));
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + o), dst + i * 512, 16, 0, 0);
+      }
+    }
+  }
+};
+// at most VM direct loads of this wavefront are still under way
+template <int VM>
+__device__ __forceinline__ void loads_wait() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((VM & 15) | ((VM >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+}
+
+// V^T fragment of 32 keys x 16 dims: lane (dim l % 16, group l / 16) gets its dim of keys 4 group .. + 3 of both 16-key tiles.
+template <int D>
+__device__ __forceinline__ void trn_issue16(TrnRegs& r, const bf16_t* tile, int dim0, int s) {
+  const int lane = threadIdx.x & 63, i = lane & 15;
+  const int row = 4 * (lane >> 4) + (i >> 2), col = dim0 + 4 * (i & 3);      // rows 16 apart have the same swizzle: both offsets are constants
+  const lds_bf16_t* t3 = (const lds_bf16_t*)tile;
+  const unsigned at = static_cast<unsigned>(reinterpret_cast<uintptr_t>(t3 + nat_off<D>(row, col >> 3) + (col & 7)));
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(r.lo) : "v"(at), "i"(s * 64 * D) : "memory");
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(r.hi) : "v"(at), "i"(s * 64 * D + 32 * D) : "memory");
+}
+// maximum over the four 16-lane groups (a row's keys are spread over them), in every lane
+__device__ __forceinline__ float groups_max(float v) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+__device__ __forceinline__ float groups_sum(float v) {
+  const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// State of the NR x 16 rows of a wavefront.
+template <int DV, int NR>
+struct RowState {
+  floatx4 o[NR][DV / 16];
+  float m[NR], l[NR];      // running reference of raw scores; this lane's share of the sum of exponentials
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      m[c] = -INFINITY;
+      l[c] = 0.f;
+#pragma unroll
+      for (int u = 0; u < DV / 16; ++u) o[c][u] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+};
+
+// One tile of KT keys.  left[c]: keys of this tile that the lane's row of column group c sees (any value: beyond KT all, below 1 none);
+// whole: every row sees all of the tile.  keep: where the scores of the lane's rows go (rows keep_pitch apart per column group; null: nowhere),
+// for the rows that `kept` has a bit for.
+template <int DQ, int DV, int NR, int KT>
+__device__ __forceinline__ void prefix_tile(const bf16_t* Kt, const bf16_t* Vt, const bf16x8_t (&qf)[NR][DQ / 32], RowState<DV, NR>& st, float sc,
+                                            bool whole, const int (&left)[NR], float* keep, int keep_pitch, unsigned kept) {
+  const int lane = threadIdx.x & 63, grp = lane >> 4, l16 = lane & 15;
+  floatx4 s[NR][KT / 16];
+  // Key fragments in groups of at most eight, all of a group read in front of its products, and products of the same 32 dims side by side: left
+  // to itself the compiler reads and waits for two fragments at a time and lets each product wait for the one before it.
+  constexpr int TG = KT / 16 < 8 / (DQ / 32) ? KT / 16 : 8 / (DQ / 32);
+#pragma unroll
+  for (int t0 = 0; t0 < KT / 16; t0 += TG) {
+    bf16x8_t kf[TG][DQ / 32];
+#pragma unroll
+    for (int t = 0; t < TG; ++t)
+#pragma unroll
+      for (int i = 0; i < DQ / 32; ++i) kf[t][i] = *reinterpret_cast<const bf16x8_t*>(Kt + nat_off<DQ>(16 * (t0 + t) + l16, 4 * i + grp));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < DQ / 32; ++i)
+#pragma unroll
+      for (int t = 0; t < TG; ++t)
+#pragma unroll
+        for (int c = 0; c < NR; ++c)
+          s[c][t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][i], qf[c][i], i == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[c][t0 + t], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (!whole) {
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+#pragma unroll
+      for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[c][t][r] = 16 * t + 4 * grp + r < left[c] ? s[c][t][r] : -INFINITY;
+  }
+  if (keep) {
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+      if ((kept >> c) & 1u) {
+#pragma unroll
+        for (int t = 0; t < KT / 16; ++t) {
+          floatx4 x;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) x[r] = s[c][t][r] * sc;
+          *reinterpret_cast<floatx4*>(keep + static_cast<long long>(c) * 16 * keep_pitch + 16 * t + 4 * grp) = x;
+        }
+      }
+  }
+  // The reference only has to keep the exponentials in range: it moves, and the accumulators are rescaled, when some row's maximum has grown
+  // by more than RESCALE_LOG2 binades since it was set (or the row sees its first key).
+  bool grown = false;
+  float m_new[NR];
+#pragma unroll
+  for (int c = 0; c < NR; ++c) {
+    float mx = s[c][0][0];
+#pragma unroll
+    for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[c][t][r]);
+    m_new[c] = fmaxf(st.m[c], groups_max(mx));
+    grown |= (m_new[c] - st.m[c]) * sc > RESCALE_LOG2;      // the first key: infinitely
+  }
+  if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const float alpha = st.m[c] == m_new[c] ? 1.f : __builtin_amdgcn_exp2f((st.m[c] - m_new[c]) * sc);
+      st.m[c] = m_new[c];
+      st.l[c] *= alpha;
+#pragma unroll
+      for (int u = 0; u < DV / 16; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) st.o[c][u][r] *= alpha;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < NR; ++c) {
+    const float msc = (st.m[c] == -INFINITY ? 0.f : st.m[c]) * sc;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[c][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][t][r], sc, -msc));
+        sum += s[c][t][r];
+      }
+    st.l[c] += sum;
+  }
+#pragma unroll
+  for (int i = 0; i < KT / 32; ++i) {
+    TrnRegs vr[DV / 16];
+#pragma unroll
+    for (int u = 0; u < DV / 16; ++u) trn_issue16<DV>(vr[u], Vt, 16 * u, i);
+    bf16x8_t pf[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const floatx8 p = {s[c][2 * i][0], s[c][2 * i][1], s[c][2 * i][2], s[c][2 * i][3], s[c][2 * i + 1][0], s[c][2 * i + 1][1], s[c][2 * i + 1][2], s[c][2 * i + 1][3]};
+      pf[c] = __builtin_convertvector(p, bf16x8_t);
+    }
+    trn_wait();
+#pragma unroll
+    for (int u = 0; u < DV / 16; ++u) {
+      const bf16x8_t vf = trn_frag(vr[u]);
+#pragma unroll
+      for (int c = 0; c < NR; ++c) st.o[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], st.o[c][u], 0, 0, 0);
+    }
+  }
+}
+
+// What an item is.
+struct Item {
+  int hk, b;            // key/value head; request of its own keys (-1: none)
+  int row0, n_rows;     // rows of the head
+  int slot;
+  int t0, t1, split;    // key tiles t0 .. t1 - 1; those from `split` on are own tiles
+  int own_n;            // own rows that may be read
+};
+template <int KT>
+__device__ __forceinline__ bool prefix_item(const PrefixArgs& a, int row_tile, Item& it) {
+  int id = blockIdx.x;
+  if (id < a.p_items) {
+    const int chunk = id / (a.p_row_tiles * a.h_kv), r = id - chunk * (a.p_row_tiles * a.h_kv);
+    it.hk = r / a.p_row_tiles;
+    it.b = -1;
+    it.row0 = (r - it.hk * a.p_row_tiles) * row_tile;
+    it.n_rows = min(row_tile, a.rows - it.row0);
+    it.slot = chunk;
+    it.t0 = chunk * a.p_chunk;
+    it.t1 = min(it.t0 + a.p_chunk, a.p_tiles);
+    it.split = a.p_tiles;
+    it.own_n = 0;
+    return true;
+  }
+  id -= a.p_items;
+  const int per = a.o_chunks * a.o_row_tiles;
+  const int bh = id / per, r = id - bh * per, chunk = r / a.o_row_tiles, rt = r - chunk * a.o_row_tiles;
+  it.b = bh / a.h_kv;
+  it.hk = bh - it.b * a.h_kv;
+  const int first = rt * row_tile;
+  it.n_rows = min(row_tile, a.own_rows - first);
+  it.row0 = it.b * a.own_rows + first;
+  it.slot = (a.joint ? 0 : a.p_chunks) + chunk;
+  it.split = a.joint ? a.p_tiles : 0;
+  const int n = own_len(a, it.b);
+  it.own_n = own_visible(n, a.L, (first + it.n_rows - 1) / a.g);      // of the last row
+  it.t0 = chunk * a.o_chunk;
+  it.t1 = min(it.t0 + a.o_chunk, it.split + (it.own_n + KT - 1) / KT);
+  return it.t0 < it.t1 || a.slots == 0;      // without slots the item writes its rows even if they see nothing
+}
+// Kept scores of own keys j .. j + 3 for four rows from r0 on (rows beyond the last: the last one's).
+struct PrefixScores { floatx4 x[4]; };
+__device__ __forceinline__ PrefixScores prefix_scores(const PrefixArgs& a, long long bh, int r0, int j) {
+  const float* const scores = a.scores + bh * a.own_rows * a.own_pad + j;
+  PrefixScores s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s.x[i] = *reinterpret_cast<const floatx4*>(scores + static_cast<long long>(min(r0 + i, a.own_rows - 1)) * a.own_pad);
+  return s;
+}
+// Accumulated weights of own keys j0 .. j0 + 3, j0 + step .. of request and head bh, from the kept scores of its rows: w_out = w_in + sum over the
+// rows of exp2(score - lse2).  early: prefix_scores() of rows 0 .. 3 and key j0.
+__device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, PrefixScores early, const float* lse2, int n, int j0, int step) {
+  for (int j = j0; j < n; j += step) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) was[e] = a.w_in ? a.w_in[bh * a.cap + min(j + e, n - 1)] : 0.f;
+    for (int r = 0; r < a.own_rows; r += 4) {
+      const PrefixScores s = r == 0 && j == j0 ? early : prefix_scores(a, bh, r, j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float ref = r + i < a.own_rows ? lse2[r + i] : INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(s.x[i][e] - ref);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < n) a.w_out[bh * a.cap + j + e] = was[e] + sum[e];
+  }
+}
+
+// Key tiles of an item, stages of LDS buffers and their bytes.  Shared tiles have 64 keys; a wavefront's own ones 32, so that two stages for four
+// wavefronts take as much as four stages of shared tiles.
+template <int DQ, int DV, int NR, bool SHARE, int NB>
+struct PrefixShape {
+  static constexpr int KT = SHARE ? 64 : 32;
+  static constexpr int loop = (SHARE ? 1 : 4) * NB * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * NR * (DV * 16 + 32) + NR * 16) * 4;
+  static constexpr int lds = loop > join ? loop : join;
+};
+
+// SHARE: the four wavefronts take NR * 16 rows each and share every key tile.  Otherwise they share the item's rows (at most NR * 16) and take
+// the key tiles in turn, from LDS buffers of their own without a barrier, and join at the end.  NB stages: NB - 1 tiles are on their way.
+template <int DQ, int DV, int NR, bool SHARE, int NB>
+__device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const lds_all) {
+  constexpr int KT = PrefixShape<DQ, DV, NR, SHARE, NB>::KT, WAVES = SHARE ? 4 : 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4, l16 = lane & 15;
+  Item it;
+  if (!prefix_item<KT>(a, (SHARE ? 4 : 1) * NR * 16, it)) return;
+  bf16_t* const buf = lds_all + (SHARE ? 0 : wave * NB * KT * (DQ + DV));      // [NB][K tile, V tile]
+
+  KvLoader<DQ, KT, WAVES> kl;
+  KvLoader<DV, KT, WAVES> vl;
+  kl.init(a.kq);
+  vl.init(a.kv);
+  const char* const pk = reinterpret_cast<const char*>(a.pk + it.hk * a.pk_sh);
+  const char* const pv = reinterpret_cast<const char*>(a.pv + it.hk * a.pv_sh);
+  const char* const ok = reinterpret_cast<const char*>(a.k + (it.b < 0 ? 0 : it.b) * a.k_sb + it.hk * a.k_sh);
+  const char* const ov = reinterpret_cast<const char*>(a.v + (it.b < 0 ? 0 : it.b) * a.v_sb + it.hk * a.v_sh);
+  const auto issue = [&](int j, int n) __attribute__((always_inline)) {
+    const bool own = j >= it.split;
+    const long long first = static_cast<long long>(own ? j - it.split : j) * KT;
+    const int valid = (own ? it.own_n : a.P) - static_cast<int>(first);
+    const long long ldk = 2 * (own ? a.k_st : a.pk_st), ldv = 2 * (own ? a.v_st : a.pv_st);
+    bf16_t* const at = buf + n * (KT * (DQ + DV));
+    kl.issue(at, (own ? ok : pk) + first * ldk, static_cast<unsigned>(ldk), valid);
+    vl.issue(at + KT * DQ, (own ? ov : pv) + first * ldv, static_cast<unsigned>(ldv), valid);
+  };
+  constexpr int STEP = SHARE ? 1 : 4;
+  const int first = it.t0 + (SHARE ? 0 : wave);
+#pragma unroll
+  for (int i = 0; i < NB - 1; ++i)
+    if (first + i * STEP < it.t1) issue(first + i * STEP, i);
+
+  // the wavefront's rows: queries straight from memory, rows and dims outside are zero
+  bf16x8_t qf[NR][DQ / 32];
+  int seen[NR];      // own keys the row sees
+#pragma unroll
+  for (int c = 0; c < NR; ++c) {
+    const int r = (SHARE ? wave * NR * 16 : 0) + c * 16 + l16, row = it.row0 + min(r, it.n_rows - 1);
+    const int token = row / a.g;
+    const bf16_t* const src = a.q + token * a.ld_q + static_cast<long long>(it.hk * a.g + (row - token * a.g)) * a.kq;
+    seen[c] = it.b < 0 ? 0 : own_visible(own_len(a, it.b), a.L, token - it.b * a.L);
+    u32x4 raw[DQ / 32];
+#pragma unroll
+    for (int i = 0; i < DQ / 32; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + min(32 * i + 8 * grp, a.kq - 8));
+#pragma unroll
+    for (int i = 0; i < DQ / 32; ++i)
+      qf[c][i] = __builtin_bit_cast(bf16x8_t, r < it.n_rows && 32 * i + 8 * grp < a.kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
+  }
+  int least = seen[0];
+#pragma unroll
+  for (int c = 1; c < NR; ++c) least = min(least, seen[c]);
+  least = static_cast<int>(wave_umin(static_cast<uint32_t>(least)));      // own keys that every row sees
+
+  // scores of own keys are kept by the items that have all rows of a request (SHARE: the call weighs them in a pass of its own)
+  float* const keep = !SHARE && a.scores && it.b >= 0 ? a.scores + (static_cast<long long>(it.b * a.h_kv + it.hk) * a.own_rows + l16) * a.own_pad : nullptr;
+  unsigned kept = 0u;
+#pragma unroll
+  for (int c = 0; c < NR; ++c) kept |= c * 16 + l16 < it.n_rows ? 1u << c : 0u;
+
+  RowState<DV, NR> st;
+  st.init();
+  int cur = 0;
+  for (int j = first; j < it.t1; j += STEP) {
+    // of the operations issued since this tile's loads, at least those of the NB - 2 tiles behind it are loads that may still be under way
+    if (NB > 2 && j + (NB - 2) * STEP < it.t1) loads_wait<(NB - 2) * (KvLoader<DQ, KT, WAVES>::PER + KvLoader<DV, KT, WAVES>::PER)>();
+    else stream_wait();
+    if (SHARE) __syncthreads();
+    if (j + (NB - 1) * STEP < it.t1) issue(j + (NB - 1) * STEP, cur == 0 ? NB - 1 : cur - 1);
+    const bool own = j >= it.split;
+    const int k0 = (own ? j - it.split : j) * KT;
+    int left[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) left[c] = (own ? seen[c] : a.P) - k0;
+    const bf16_t* const at = buf + cur * (KT * (DQ + DV));
+    prefix_tile<DQ, DV, NR, KT>(at, at + KT * DQ, qf, st, a.sc, k0 + KT <= (own ? least : a.P), left, own && keep ? keep + k0 : nullptr, a.own_pad, kept);
+    cur = cur + 1 == NB ? 0 : cur + 1;
+  }
+#pragma unroll
+  for (int c = 0; c < NR; ++c) st.l[c] = groups_sum(st.l[c]);
+
+  // this lane's four dims of block u of row r: normalised into the output, or a piece for the join
+  const auto write = [&](int c, int u, const floatx4& acc, float m, float l, bool with_ml) __attribute__((always_inline)) {
+    const int r = (SHARE ? wave * NR * 16 : 0) + c * 16 + l16, row = it.row0 + r;
+    if (r >= it.n_rows) return;
+    if (a.slots == 0) {
+      const int token = row / a.g, head = it.hk * a.g + (row - token * a.g);
+      if (16 * u < a.kv) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        floatx4 f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = acc[i] * inv;
+        *reinterpret_cast<bf16x4_t*>(a.o + token * a.ld_o + static_cast<long long>(head) * a.kv + 16 * u + 4 * grp) = __builtin_convertvector(f, bf16x4_t);
+      }
+      if (with_ml && a.lse && grp == 0) {
+        const int b = token / a.L;
+        a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l > 0.f ? (m * a.sc + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+      }
+    } else {
+      const long long at = (static_cast<long long>(it.hk) * a.rows + row) * a.slots + it.slot;
+      if (16 * u < a.kv) *reinterpret_cast<floatx4*>(a.part_o + at * a.kv + 16 * u + 4 * grp) = acc;
+      if (with_ml && grp == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m * a.sc, l};
+    }
+  };
+  if (SHARE) {
+#pragma unroll
+    for (int c = 0; c < NR; ++c)
+#pragma unroll
+      for (int u = 0; u < DV / 16; ++u) write(c, u, st.o[c][u], st.m[c], st.l[c], u == 0);
+  } else {
+    __syncthreads();
+    float* const part = reinterpret_cast<float*>(lds_all);      // [4][NR][DV / 16][4][64]
+    float* const ms = part + 4 * NR * DV * 16;                  // [4][NR][16] each
+    float* const ls = ms + 4 * NR * 16;
+    float* const lse2 = ls + 4 * NR * 16;                       // [NR][16]
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+#pragma unroll
+      for (int u = 0; u < DV / 16; ++u)
+        *reinterpret_cast<floatx4*>(part + (((wave * NR + c) * (DV / 16) + u) * 64 + lane) * 4) = st.o[c][u];
+      if (grp == 0) {
+        ms[(wave * NR + c) * 16 + l16] = st.m[c];
+        ls[(wave * NR + c) * 16 + l16] = st.l[c];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      float m_all = ms[c * 16 + l16], al[4], l_all = 0.f;
+#pragma unroll
+      for (int w = 1; w < 4; ++w) m_all = fmaxf(m_all, ms[(w * NR + c) * 16 + l16]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float m = ms[(w * NR + c) * 16 + l16];
+        al[w] = m == m_all ? (m == -INFINITY ? 0.f : 1.f) : __builtin_amdgcn_exp2f((m - m_all) * a.sc);
+        l_all += al[w] * ls[(w * NR + c) * 16 + l16];
+      }
+#pragma unroll
+      for (int u0 = 0; u0 < DV / 16; u0 += 4) {
+        const int u = u0 + wave;
+        if (u >= DV / 16) break;
+        floatx4 f = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const floatx4 x = *reinterpret_cast<const floatx4*>(part + (((w * NR + c) * (DV / 16) + u) * 64 + lane) * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] += al[w] * x[i];
+        }
+        write(c, u, f, m_all, l_all, u == 0);
+      }
+      if (a.slots == 0 && wave == 0 && grp == 0) lse2[c * 16 + l16] = l_all > 0.f ? m_all * a.sc + __builtin_amdgcn_logf(l_all) : INFINITY;
+    }
+    if (a.slots == 0 && keep) {      // the item has seen all of its rows' keys: weights from the scores it kept
+      __threadfence_block();
+      __syncthreads();
+      const long long bh = static_cast<long long>(it.b) * a.h_kv + it.hk;
+      if (it.own_n > 0) prefix_weigh(a, bh, prefix_scores(a, bh, 0, min(static_cast<int>(threadIdx.x) * 4, a.own_pad - 4)), lse2, it.own_n, threadIdx.x * 4, 1024);
+    }
+  }
+}
+
+// Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64 or 128, 16 or 32 a wavefront.
+enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3 };
+template <int DQ, int DV, int ROWS, int NB>
+__device__ __forceinline__ void prefix_kind(const PrefixArgs& a, bf16_t* lds) {
+  prefix_rows<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>(a, lds);
+}
+// OWN: rows of the items of a request; PREFIX: of those of the prefix alone, in front of them in the grid (the same: all items are of one kind).
+// Shared tiles have four stages beside own ones (whose LDS is there anyway), else two, for more workgroups on a compute unit.
+template <int DQ, int DV, int OWN, int PREFIX>
+struct PrefixKernel {
+  static constexpr int NB_P = 4, NB_O = 2;
+  template <int ROWS, int NB> static constexpr int lds_of() { return PrefixShape<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>::lds; }
+  static constexpr int own = lds_of<OWN, NB_O>(), pre = OWN == PREFIX ? 0 : lds_of<PREFIX, PREFIX >= ROWS_64 ? NB_P : NB_O>();
+  static constexpr int lds = own > pre ? own : pre;
+};
+// Two wavefronts a SIMD at least: the register file then has no accumulation half, and the scores need no moves between the halves.
+template <int DQ, int DV, int OWN, int PREFIX>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_attn_kernel(const PrefixArgs a) {
+  typedef PrefixKernel<DQ, DV, OWN, PREFIX> K;
+  extern __shared__ __attribute__((aligned(16))) bf16_t lds_all[];      // one object: see attn.hip
+  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_kind<DQ, DV, PREFIX, PREFIX >= ROWS_64 ? K::NB_P : K::NB_O>(a, lds_all);
+  else prefix_kind<DQ, DV, OWN, K::NB_O>(a, lds_all);
+}
+
+// the pairs that are built
+#define PREFIX_KINDS(X) X(ROWS_16, ROWS_16) X(ROWS_32, ROWS_32) X(ROWS_64, ROWS_64) X(ROWS_128, ROWS_128) X(ROWS_16, ROWS_32) \
+  X(ROWS_16, ROWS_64) X(ROWS_32, ROWS_64) X(ROWS_16, ROWS_128) X(ROWS_32, ROWS_128)
+template <int DQ, int DV, int OWN, int PREFIX>
+static hipError_t prefix_launch(const PrefixArgs& a, unsigned grid, hipStream_t st) {
+  constexpr int lds = PrefixKernel<DQ, DV, OWN, PREFIX>::lds;
+  const auto kern = prefix_attn_kernel<DQ, DV, OWN, PREFIX>;
+  static LdsAttrOnce attr_once;
+  if (lds > 64 * 1024) {
+    const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, a);
+  return hipGetLastError();
+}
+template <int DQ, int DV>
+static hipError_t prefix_launch_width(const PrefixArgs& a, int own, int prefix, unsigned grid, hipStream_t st) {
+#define PREFIX_KIND(O, P) if (own == O && prefix == P) return prefix_launch<DQ, DV, O, P>(a, grid, st);
+  PREFIX_KINDS(PREFIX_KIND)
+#undef PREFIX_KIND
+  return hipErrorInvalidValue;
+}
+// by the width of the queries, a translation unit each
+hipError_t prefix_launch_32(const PrefixArgs& a, int dv, int own, int prefix, unsigned grid, hipStream_t st);
+hipError_t prefix_launch_64(const PrefixArgs& a, int dv, int own, int prefix, unsigned grid, hipStream_t st);
+hipError_t prefix_launch_128(const PrefixArgs& a, int dv, int own, int prefix, unsigned grid, hipStream_t st);

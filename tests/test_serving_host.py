@@ -46,7 +46,7 @@ BAD_CACHES = [
 def test_caches_are_refused(lib, ctx, change, code):
     c = cache(**change)
     assert lib.ecospa_prefix_attn(ctx, C.byref(c), 1, 256, 256, 512, 384, None, None, None) == code
-    assert lib.ecospa_prefix_attn_workspace_bytes(C.byref(c), 1) == 0
+    assert lib.ecospa_prefix_attn_workspace_bytes(C.byref(c), 1, 1) == 0
     assert lib.ecospa_cache_append(ctx, C.byref(c), 1, 256, 576, None, None, None, 0, 512, 256, None) == code
     if not {"pk", "pv", "P", "pk_st", "pv_st", "pk_sh", "pv_sh"} & set(change):
         assert lib.ecospa_cache_evict(ctx, C.byref(c), 256, 10, 2, C.byref(cache()), 512, None, 1024) == code
@@ -63,7 +63,7 @@ def test_attention_refusals(lib, ctx):
     assert call(q=264) == call(o=520) == call(ld_q=260) == call(ld_o=388) == B.ERR_ALIGN
     # pieces of a long prefix are joined in the workspace: none attached
     long = cache(P=1 << 16)
-    need = lib.ecospa_prefix_attn_workspace_bytes(C.byref(long), 1)
+    need = lib.ecospa_prefix_attn_workspace_bytes(C.byref(long), 1, 0)
     assert need > 0 and call(desc=long) == B.ERR_WORKSPACE
     assert lib.ecospa_set_workspace(ctx, 1 << 20, 256) == B.OK and call(desc=long) == B.ERR_WORKSPACE
     # weights without lse keep their row statistics there
