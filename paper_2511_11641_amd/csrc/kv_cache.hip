@@ -76,11 +76,12 @@ struct EvictArgs {
   int *lens_out, *idx;
   long long k_sb, k_sh, k_st, v_sb, v_sh, v_st, ko_sb, ko_sh, ko_st, vo_sb, vo_sh, vo_st;
   int B, h_kv, cap, cap_out, own_max, keep, recent, kq, kv;
+  int small;             // pieces are numbered below 2^27: their row is the high half of a product
+  unsigned per_inv;      // 2^32 / pieces of a row, rounded up
 };
 __device__ __forceinline__ int evict_len(const EvictArgs& a, int b) { return min(max(a.lens[b], 0), a.own_max); }
-__global__ __launch_bounds__(SELECT_THREADS) void cache_choose_kernel(const EvictArgs a) {
-  __shared__ SelectShared sh;
-  const int bh = blockIdx.x, b = bh / a.h_kv, n = evict_len(a, b);
+__device__ __forceinline__ void cache_choose(const EvictArgs& a, int bh, SelectShared& sh) {
+  const int b = bh / a.h_kv, n = evict_len(a, b);
   int* const idx = a.idx + static_cast<long long>(bh) * a.keep;
   if (threadIdx.x == 0 && bh == b * a.h_kv) a.lens_out[b] = min(n, a.keep);
   if (n <= a.keep) {
@@ -98,18 +99,56 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_choose_kernel(const Evic
   t.groups = 1;
   select_item_block(t, 0, sh);
 }
+__global__ __launch_bounds__(SELECT_THREADS) void cache_choose_kernel(const EvictArgs a) {
+  __shared__ SelectShared sh;
+  cache_choose(a, blockIdx.x, sh);
+}
+// Pieces `id`, id + step, .. of the kept rows of one cache, 16 bytes each, four at a time: row numbers, then rows, then stores, so that four rows of
+// a thread are on their way together.
+__device__ __forceinline__ void cache_gather(const EvictArgs& a, int bh, int n, long long id0, long long most, int step) {
+  const int b = bh / a.h_kv, hk = bh - b * a.h_kv, cq = a.kq >> 3, per = cq + (a.kv >> 3);
+  const int* const idx = a.idx + static_cast<long long>(bh) * a.keep;
+  const bf16_t* const k = a.k + b * a.k_sb + hk * a.k_sh;
+  const bf16_t* const v = a.v + b * a.v_sb + hk * a.v_sh;
+  bf16_t* const ko = a.k_out + b * a.ko_sb + hk * a.ko_sh;
+  bf16_t* const vo = a.v_out + b * a.vo_sb + hk * a.vo_sh;
+  const long long all = static_cast<long long>(n) * per, end = all < most ? all : most;
+  for (long long id = id0; id < end; id += 4ll * step) {
+    int i[4], c[4], j[4];
+    uint4 x[4];
+    float w[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long at = id + static_cast<long long>(u) * step < end ? id + static_cast<long long>(u) * step : id;
+      i[u] = static_cast<int>(a.small ? __umulhi(static_cast<unsigned>(at), a.per_inv) : at / per);
+      c[u] = static_cast<int>(at - static_cast<long long>(i[u]) * per);
+      j[u] = min(max(idx[i[u]], 0), a.cap - 1);      // whatever a list holds, nothing outside the cache is read
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      x[u] = *reinterpret_cast<const uint4*>(c[u] < cq ? k + j[u] * a.k_st + c[u] * 8 : v + j[u] * a.v_st + (c[u] - cq) * 8);
+      w[u] = c[u] == 0 && a.weights_out ? a.weights[static_cast<long long>(bh) * a.cap + j[u]] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (id + static_cast<long long>(u) * step >= end) continue;
+      *reinterpret_cast<uint4*>(c[u] < cq ? ko + i[u] * a.ko_st + c[u] * 8 : vo + i[u] * a.vo_st + (c[u] - cq) * 8) = x[u];
+      if (c[u] == 0 && a.weights_out) a.weights_out[static_cast<long long>(bh) * a.cap_out + i[u]] = w[u];
+    }
+  }
+}
 __global__ __launch_bounds__(256) void cache_gather_kernel(const EvictArgs a) {
-  const int bh = blockIdx.y, b = bh / a.h_kv, hk = bh - b * a.h_kv, n = min(evict_len(a, b), a.keep);
-  const int cq = a.kq >> 3, per = cq + (a.kv >> 3);
-  const int id = blockIdx.x * 256 + threadIdx.x, i = id / per, c = id - i * per;
-  if (i >= n) return;
-  const int j = a.idx[static_cast<long long>(bh) * a.keep + i];
-  if (c < cq)
-    *reinterpret_cast<uint4*>(a.k_out + b * a.ko_sb + hk * a.ko_sh + i * a.ko_st + c * 8) = *reinterpret_cast<const uint4*>(a.k + b * a.k_sb + hk * a.k_sh + j * a.k_st + c * 8);
-  else
-    *reinterpret_cast<uint4*>(a.v_out + b * a.vo_sb + hk * a.vo_sh + i * a.vo_st + (c - cq) * 8) =
-        *reinterpret_cast<const uint4*>(a.v + b * a.v_sb + hk * a.v_sh + j * a.v_st + (c - cq) * 8);
-  if (c == 0 && a.weights_out) a.weights_out[static_cast<long long>(bh) * a.cap_out + i] = a.weights[static_cast<long long>(bh) * a.cap + j];
+  const int bh = blockIdx.y, n = min(evict_len(a, bh / a.h_kv), a.keep);
+  const long long first = static_cast<long long>(blockIdx.x) * 1024;
+  cache_gather(a, bh, n, first + threadIdx.x, first + 1024, 256);
+}
+// Both in one launch: the workgroup that chose the rows of a cache moves them.
+__global__ __launch_bounds__(SELECT_THREADS) void cache_evict_kernel(const EvictArgs a) {
+  __shared__ SelectShared sh;
+  cache_choose(a, blockIdx.x, sh);
+  __threadfence_block();
+  __syncthreads();
+  cache_gather(a, blockIdx.x, min(evict_len(a, blockIdx.x / a.h_kv), a.keep), threadIdx.x, 1ll << 62, SELECT_THREADS);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -167,13 +206,21 @@ extern "C" int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src, cons
   a.ko_sb = d.k_sb; a.ko_sh = d.k_sh; a.ko_st = d.k_st; a.vo_sb = d.v_sb; a.vo_sh = d.v_sh; a.vo_st = d.v_st;
   a.B = src->B; a.h_kv = src->h_kv; a.cap = src->cap; a.cap_out = d.cap; a.own_max = src->own_max; a.keep = keep; a.recent = recent;
   a.kq = src->kp_qk; a.kv = src->kp_vo;
-  const int groups = a.B * a.h_kv;
+  const int groups = a.B * a.h_kv, per = (a.kq + a.kv) / 8;
+  const long long n = static_cast<long long>(keep < a.own_max ? keep : a.own_max) * per;      // pieces of a cache
+  if ((n + 1023) / 1024 > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
+  a.small = n < 1 << 27;
+  a.per_inv = static_cast<unsigned>(((1ll << 32) + per - 1) / per);
+  // Small caches: the launch saved outweighs the copying that one workgroup a cache does more slowly.
+  if (n * 16 <= 128 * 1024) {
+    hipLaunchKernelGGL(cache_evict_kernel, dim3(groups), dim3(SELECT_THREADS), 0, ctx->stream, a);
+    ECOSPA_CHECK_LAUNCH(ctx, "cache_evict_kernel");
+    return ECOSPA_OK;
+  }
   hipLaunchKernelGGL(cache_choose_kernel, dim3(groups), dim3(SELECT_THREADS), 0, ctx->stream, a);
   ECOSPA_CHECK_LAUNCH(ctx, "cache_choose_kernel");
-  const long long n = static_cast<long long>(keep < a.own_max ? keep : a.own_max) * ((a.kq + a.kv) / 8);
-  if (n > 0x7fffffffll - 256) return ECOSPA_ERR_SHAPE;
   if (n > 0) {
-    hipLaunchKernelGGL(cache_gather_kernel, dim3(static_cast<unsigned>((n + 255) / 256), groups), dim3(256), 0, ctx->stream, a);
+    hipLaunchKernelGGL(cache_gather_kernel, dim3(static_cast<unsigned>((n + 1023) / 1024), groups), dim3(256), 0, ctx->stream, a);
     ECOSPA_CHECK_LAUNCH(ctx, "cache_gather_kernel");
   }
   return ECOSPA_OK;

@@ -376,11 +376,13 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
   for (int c = 1; c < NR; ++c) least = min(least, seen[c]);
   least = static_cast<int>(wave_umin(static_cast<uint32_t>(least)));      // own keys that every row sees
 
-  // scores of own keys are kept by the items that have all rows of a request (SHARE: the call weighs them in a pass of its own)
-  float* const keep = !SHARE && a.scores && it.b >= 0 ? a.scores + (static_cast<long long>(it.b * a.h_kv + it.hk) * a.own_rows + l16) * a.own_pad : nullptr;
+  // scores of own keys are kept where the call wants weights (then an item has all rows of its request)
+  const int first_row = SHARE ? wave * NR * 16 : 0;
+  const bool idle = first_row >= it.n_rows;      // a wavefront without rows only loads
+  float* const keep = a.scores && it.b >= 0 ? a.scores + (static_cast<long long>(it.b * a.h_kv + it.hk) * a.own_rows + first_row + l16) * a.own_pad : nullptr;
   unsigned kept = 0u;
 #pragma unroll
-  for (int c = 0; c < NR; ++c) kept |= c * 16 + l16 < it.n_rows ? 1u << c : 0u;
+  for (int c = 0; c < NR; ++c) kept |= first_row + c * 16 + l16 < it.n_rows ? 1u << c : 0u;
 
   RowState<DV, NR> st;
   st.init();
@@ -391,14 +393,15 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
     else stream_wait();
     if (SHARE) __syncthreads();
     if (j + (NB - 1) * STEP < it.t1) issue(j + (NB - 1) * STEP, cur == 0 ? NB - 1 : cur - 1);
+    cur = cur + 1 == NB ? 0 : cur + 1;
+    if (idle) continue;
     const bool own = j >= it.split;
     const int k0 = (own ? j - it.split : j) * KT;
     int left[NR];
 #pragma unroll
     for (int c = 0; c < NR; ++c) left[c] = (own ? seen[c] : a.P) - k0;
-    const bf16_t* const at = buf + cur * (KT * (DQ + DV));
+    const bf16_t* const at = buf + (cur == 0 ? NB - 1 : cur - 1) * (KT * (DQ + DV));
     prefix_tile<DQ, DV, NR, KT>(at, at + KT * DQ, qf, st, a.sc, k0 + KT <= (own ? least : a.P), left, own && keep ? keep + k0 : nullptr, a.own_pad, kept);
-    cur = cur + 1 == NB ? 0 : cur + 1;
   }
 #pragma unroll
   for (int c = 0; c < NR; ++c) st.l[c] = groups_sum(st.l[c]);
@@ -490,12 +493,12 @@ __device__ __forceinline__ void prefix_kind(const PrefixArgs& a, bf16_t* lds) {
   prefix_rows<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>(a, lds);
 }
 // OWN: rows of the items of a request; PREFIX: of those of the prefix alone, in front of them in the grid (the same: all items are of one kind).
-// Shared tiles have four stages beside own ones (whose LDS is there anyway), else two, for more workgroups on a compute unit.
+// Shared tiles have four stages beside own ones (whose LDS is there anyway), else few enough for several workgroups on a compute unit.
 template <int DQ, int DV, int OWN, int PREFIX>
 struct PrefixKernel {
-  static constexpr int NB_P = 4, NB_O = 2;
+  static constexpr int NB_S = DQ + DV <= 128 && OWN == ROWS_64 ? 3 : 2, NB_O = OWN >= ROWS_64 ? NB_S : 2, NB_P = PREFIX < ROWS_64 ? 2 : (OWN >= ROWS_64 ? NB_S : 4);
   template <int ROWS, int NB> static constexpr int lds_of() { return PrefixShape<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>::lds; }
-  static constexpr int own = lds_of<OWN, NB_O>(), pre = OWN == PREFIX ? 0 : lds_of<PREFIX, PREFIX >= ROWS_64 ? NB_P : NB_O>();
+  static constexpr int own = lds_of<OWN, NB_O>(), pre = OWN == PREFIX ? 0 : lds_of<PREFIX, NB_P>();
   static constexpr int lds = own > pre ? own : pre;
 };
 // Two wavefronts a SIMD at least: the register file then has no accumulation half, and the scores need no moves between the halves.
@@ -503,13 +506,13 @@ template <int DQ, int DV, int OWN, int PREFIX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_attn_kernel(const PrefixArgs a) {
   typedef PrefixKernel<DQ, DV, OWN, PREFIX> K;
   extern __shared__ __attribute__((aligned(16))) bf16_t lds_all[];      // one object: see attn.hip
-  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_kind<DQ, DV, PREFIX, PREFIX >= ROWS_64 ? K::NB_P : K::NB_O>(a, lds_all);
+  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_kind<DQ, DV, PREFIX, K::NB_P>(a, lds_all);
   else prefix_kind<DQ, DV, OWN, K::NB_O>(a, lds_all);
 }
 
 // the pairs that are built
 #define PREFIX_KINDS(X) X(ROWS_16, ROWS_16) X(ROWS_32, ROWS_32) X(ROWS_64, ROWS_64) X(ROWS_128, ROWS_128) X(ROWS_16, ROWS_32) \
-  X(ROWS_16, ROWS_64) X(ROWS_32, ROWS_64) X(ROWS_16, ROWS_128) X(ROWS_32, ROWS_128)
+  X(ROWS_16, ROWS_64) X(ROWS_32, ROWS_64) X(ROWS_16, ROWS_128) X(ROWS_32, ROWS_128) X(ROWS_64, ROWS_128)
 template <int DQ, int DV, int OWN, int PREFIX>
 static hipError_t prefix_launch(const PrefixArgs& a, unsigned grid, hipStream_t st) {
   constexpr int lds = PrefixKernel<DQ, DV, OWN, PREFIX>::lds;

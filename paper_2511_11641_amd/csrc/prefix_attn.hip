@@ -1,6 +1,8 @@
 // Attention over a shared prefix and own caches: the join of the pieces, accumulated weights, and the entry points (kernels: prefix_attn.h).
 #include "prefix_attn.h"
 
+#include <cmath>
+
 // ---------------------------------------------------------------------------------------------
 // Join.  Threads are (piece, four dims): a thread weighs its pieces against the maximum of its own, four of them asked for at a time, before it is
 // known how many there are (what counts is how many latencies follow on each other).  FEW pieces: W threads take a row by themselves.  Otherwise a
@@ -187,7 +189,7 @@ struct PrefixPlan {
 // prompts of 16 x 509 tokens; the unused rows of a tile cost as much).
 struct ItemCost { double step, item; };
 static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double active) {
-  const double keys = keys_of(kind) * tiles_at_once(kind), per_cu = active < 256 ? 1 : active / 256;
+  const double keys = keys_of(kind) * tiles_at_once(kind), per_cu = std::ceil(active / 256);
   const double memory = active * keys * (a.kq + a.kv) * 2 / 5500, compute = per_cu * rows_of(kind) * keys * (0.02 + 0.0005 * (p.dq + p.dv));
   double step = 900;
   if (memory > step) step = memory;
@@ -224,7 +226,7 @@ static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
 }
 // Items of the prefix for the rows of all requests, and items of own keys.
 static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool set) {
-  const int prefix = kind_of(a.rows), kt = keys_of(p.own), at_once = tiles_at_once(p.own), kt_p = keys_of(prefix), at_once_p = tiles_at_once(prefix);
+  const int prefix = kind_of(a.rows) < p.own ? p.own : kind_of(a.rows), kt = keys_of(p.own), at_once = tiles_at_once(p.own), kt_p = keys_of(prefix), at_once_p = tiles_at_once(prefix);
   const long long row_tiles = ceil_div(a.rows, rows_of(prefix)), pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles;
   const long long p_steps = ceil_div(ceil_div(a.P, kt_p), at_once_p), o_steps = ceil_div(ceil_div(a.own_max, kt), at_once);
   double best = 0;
@@ -270,11 +272,22 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   const long long resident_joint = p.own >= ROWS_64 ? resident_128 : resident_own;
   // Rows of a request that fill a tile of their own, a batch of one or no prefix: nothing to gain by putting requests together.
   const bool only_joint = a.B == 1 || a.P == 0 || p.own >= ROWS_64;
-  if (only_joint || plan_joint(a, p, resident_joint, false) <= plan_apart(a, p, resident_own, false)) plan_joint(a, p, resident_joint, true);
-  else plan_apart(a, p, resident_own, true);
+  // Wide heads apart: own tiles for every wavefront take so much LDS that one workgroup is left to a compute unit; shared tiles leave two, and a
+  // wavefront with the few rows keeps up with memory (12 x 5 tokens on 8191, 96 and 128 dims: 49 -> 44 us; 64 and 64 dims: no difference).
+  const int own = p.own, apart_own = p.dq + p.dv > 128 ? ROWS_64 : p.own;
+  const double joint = only_joint ? 0 : plan_joint(a, p, resident_joint, false);
+  p.own = apart_own;
+  if (!only_joint && plan_apart(a, p, apart_own == ROWS_64 ? resident_128 : resident_own, false) < joint) {
+    plan_apart(a, p, apart_own == ROWS_64 ? resident_128 : resident_own, true);
+  } else {
+    p.own = own;
+    plan_joint(a, p, resident_joint, true);
+  }
+  // the kernels cut the keys as the plan did
+  if (a.p_tiles != ceil_div(a.P, keys_of(p.prefix)) || p.prefix < p.own) return false;
   // The weights need every own score against a sum that is complete only at the end.  Kept scores are written and read, 8 bytes a row and key;
   // without them the keys are read a second time, 2 kp_qk bytes a key, in a launch of its own.
-  const bool keep = weights && p.own <= ROWS_32 && a.own_max > 0 && 4 * a.own_rows <= a.kq;
+  const bool keep = weights && a.own_rows <= 32 && a.own_max > 0 && 4 * a.own_rows <= a.kq;
   const long long weigh = keep && a.slots ? static_cast<long long>(a.B) * a.h_kv * ceil_div(a.own_max, 1024) : 0;
   const long long grid = a.p_items + static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles * a.o_chunks;
   if (grid > 0x7fffffffll || rows + weigh > 0x7fffffffll || static_cast<long long>(a.p_chunks) * a.p_row_tiles * a.h_kv > 0x7fffffffll) return false;
@@ -283,7 +296,7 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   const size_t pieces = static_cast<size_t>(rows) * a.slots;
   p.part_o = pieces * a.kv * sizeof(float);
   p.part_ml = pieces * 2 * sizeof(float);
-  a.own_pad = static_cast<int>(ceil_div(a.own_max, 32) * 32);
+  a.own_pad = static_cast<int>(ceil_div(a.own_max, 64) * 64);
   p.scores = keep ? static_cast<size_t>(rows) * a.own_pad * sizeof(float) : 0;
   p.lse = weights && !keep ? static_cast<size_t>(a.B) * a.L * a.h * sizeof(float) : 0;
   return true;
@@ -334,6 +347,17 @@ static int prefix_args(const ecospa_cache* c, int L, PrefixArgs& a, PrefixPlan& 
   a.own_rows = L * a.g;
   a.rows = c->B * a.own_rows;
   return prefix_plan(a, p, weights) ? ECOSPA_OK : ECOSPA_ERR_SHAPE;
+}
+
+// How the launches cut a call (for tests): the fields in the order below; 0 where the call would be refused.
+int prefix_attn_cut(const ecospa_cache& cache, int L, int weights, int* out) {
+  PrefixArgs a;
+  PrefixPlan p;
+  if (ecospa_cache_check(&cache) != ECOSPA_OK || prefix_args(&cache, L, a, p, weights != 0) != ECOSPA_OK) return 0;
+  const int fields[] = {a.joint, a.p_tiles, a.p_chunks, a.p_chunk, a.p_row_tiles, a.p_items, a.o_chunks, a.o_chunk, a.o_row_tiles, a.slots, p.own, p.prefix,
+                        static_cast<int>(p.grid), static_cast<int>(p.weigh), a.own_pad, p.scores > 0};
+  for (size_t i = 0; i < sizeof(fields) / sizeof(fields[0]); ++i) out[i] = fields[i];
+  return static_cast<int>(sizeof(fields) / sizeof(fields[0]));
 }
 
 extern "C" size_t ecospa_prefix_attn_workspace_bytes(const ecospa_cache* cache, int L, int with_weights) {

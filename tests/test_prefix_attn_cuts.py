@@ -1,0 +1,117 @@
+"""How an attention call over a shared prefix is cut into items (csrc/prefix_attn.hip), asked of the host function that the launches go by, and decoded
+here as the kernels decode a workgroup's number: every row meets every key that it sees exactly once, no tile starts behind the keys, and the pieces
+that the join reads are the ones that items wrote.  Nothing is launched; addresses are made up."""
+import ctypes as C
+import random
+
+import pytest
+
+from paper_2511_11641_amd import binding as B
+
+FIELDS = ("joint", "p_tiles", "p_chunks", "p_chunk", "p_row_tiles", "p_items", "o_chunks", "o_chunk", "o_row_tiles", "slots", "own", "prefix", "grid", "weigh", "own_pad", "keep")
+ROWS, KEYS, AT_ONCE = (16, 32, 64, 128), (32, 32, 64, 64), (4, 4, 1, 1)
+PAIRS = {(0, 0), (1, 1), (2, 2), (3, 3), (0, 1), (0, 2), (1, 2), (0, 3), (1, 3), (2, 3)}      # the kernels that are built
+
+
+def cut(lib, Bn, L, h, h_kv, e, f, P, own_max, weights=1):
+    c = B.Cache(B.BF16, Bn, h, h_kv, e, f, max(own_max, 1), own_max, P, 0.125, 4096, 8192, h_kv * max(own_max, 1) * e, max(own_max, 1) * e, e,
+                h_kv * max(own_max, 1) * f, max(own_max, 1) * f, f, 16384, 32768, P * e, e, P * f, f, 65536)
+    out = (C.c_int * 32)()
+    n = lib._Z15prefix_attn_cutRK12ecospa_cacheiiPi(C.byref(c), L, weights, out)
+    assert n == len(FIELDS)
+    return dict(zip(FIELDS, out[:n])), lib.ecospa_prefix_attn_workspace_bytes(C.byref(c), L, weights)
+
+
+def items(a, Bn, L, h, h_kv, P, lens):
+    """(head, first row, rows, slot, prefix keys [k0, k1), request or None, own keys [k0, k1)) of every workgroup that has something to do."""
+    g = h // h_kv
+    own_rows, rows = L * g, Bn * L * g
+    for wg in range(a["grid"]):
+        if wg < a["p_items"]:
+            tile, kt = ROWS[a["prefix"]], KEYS[a["prefix"]]
+            chunk, r = divmod(wg, a["p_row_tiles"] * h_kv)
+            hk, rt = divmod(r, a["p_row_tiles"])
+            t0, t1 = chunk * a["p_chunk"], min((chunk + 1) * a["p_chunk"], a["p_tiles"])
+            yield hk, rt * tile, min(tile, rows - rt * tile), chunk, [(j, 0) for j in range(t0, t1)], None, kt, 0
+            continue
+        tile, kt = ROWS[a["own"]], KEYS[a["own"]]
+        bh, r = divmod(wg - a["p_items"], a["o_chunks"] * a["o_row_tiles"])
+        chunk, rt = divmod(r, a["o_row_tiles"])
+        b, hk = divmod(bh, h_kv)
+        assert b < Bn
+        n_rows = min(tile, own_rows - rt * tile)
+        n = min(max(lens[b], 0), a["own_max"])
+        own_n = min(max(n - L + 1 + (rt * tile + n_rows - 1) // g, 0), n)
+        split = a["p_tiles"] if a["joint"] else 0
+        t0, t1 = chunk * a["o_chunk"], min((chunk + 1) * a["o_chunk"], split + -(-own_n // kt))
+        if t0 < t1 or a["slots"] == 0:
+            yield hk, b * own_rows + rt * tile, n_rows, (0 if a["joint"] else a["p_chunks"]) + chunk, [(j, 0) if j < split else (j - split, 1) for j in range(t0, t1)], b, kt, own_n
+
+
+def check(lib, Bn, L, h, h_kv, e, f, P, own_max, lens, weights):
+    a, need = cut(lib, Bn, L, h, h_kv, e, f, P, own_max, weights)
+    a["own_max"] = own_max
+    g = h // h_kv
+    own_rows, rows = L * g, Bn * L * g
+    assert (a["own"], a["prefix"]) in PAIRS and a["p_tiles"] == -(-P // KEYS[a["prefix"]])
+    assert ROWS[a["own"]] >= min(own_rows, 128) and a["o_row_tiles"] == -(-own_rows // ROWS[a["own"]])
+    assert a["own_pad"] >= -(-own_max // KEYS[a["own"]]) * KEYS[a["own"]] and a["own_pad"] % 4 == 0
+    if a["keep"]:
+        assert a["o_row_tiles"] == 1 and own_rows <= 32 and (a["weigh"] > 0) == (a["slots"] > 0)
+    assert need >= h_kv * rows * a["slots"] * (f + 2) * 4 + (h_kv * rows * a["own_pad"] * 4 if a["keep"] else 0)
+    seen = [[0] * rows for _ in range(h_kv)]             # keys that a row met
+    wrote = [[set() for _ in range(rows)] for _ in range(h_kv)]
+    tiles = [set() for _ in range(h_kv)]
+    for hk, row0, n_rows, slot, todo, b, kt, own_n in items(a, Bn, L, h, h_kv, P, lens):
+        assert 0 <= hk < h_kv and 0 <= row0 and 1 <= n_rows and row0 + n_rows <= rows and (a["slots"] == 0 or 0 <= slot < a["slots"])
+        for row in range(row0, row0 + n_rows):
+            assert slot not in wrote[hk][row]
+            wrote[hk][row].add(slot)
+        for j, own in todo:
+            assert j * kt < (own_n if own else P), "a tile behind the keys"
+            for row in range(row0, row0 + n_rows):
+                if own:
+                    n = min(max(lens[b], 0), own_max)
+                    vis = min(max(n - L + 1 + (row - b * own_rows) // g, 0), n)
+                    seen[hk][row] += min(max(vis - j * kt, 0), kt)
+                else:
+                    seen[hk][row] += min(P - j * kt, kt)
+                assert (row, own, j) not in tiles[hk]
+                tiles[hk].add((row, own, j))
+    for row in range(rows):
+        b, r = divmod(row, own_rows)
+        n = min(max(lens[b], 0), own_max)
+        want = P + min(max(n - L + 1 + r // g, 0), n)
+        # pieces as the join counts them
+        tile = ROWS[a["own"]]
+        last = min(r // tile * tile + tile, own_rows) - 1
+        own_n = min(max(n - L + 1 + last // g, 0), n)
+        own_tiles = -(-own_n // KEYS[a["own"]]) + (a["p_tiles"] if a["joint"] else 0)
+        pieces = (0 if a["joint"] else a["p_chunks"]) + -(-own_tiles // a["o_chunk"])
+        for hk in range(h_kv):
+            assert seen[hk][row] == want
+            assert a["slots"] == 0 or wrote[hk][row] == set(range(pieces)) and pieces <= a["slots"]
+            assert a["slots"] > 0 or wrote[hk][row]
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return B.load()
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_every_row_meets_every_key_once(lib, seed):
+    rng = random.Random(seed)
+    h, h_kv = rng.choice(((1, 1), (4, 4), (8, 2), (16, 16), (8, 1), (32, 2), (6, 3)))
+    L = rng.choice((1, 1, 1, 2, 5, 17, 40, 130))
+    Bn = rng.choice((1, 2, 3, 5, 16, 33) if L < 17 else (1, 2, 3))
+    P, own_max = rng.choice((0, 1, 31, 33, 64, 65, 500, 4097)), rng.choice((0, 1, 32, 33, 100, 700))
+    lens = [rng.choice((0, 1, own_max // 2, own_max, own_max + 3, -2)) for _ in range(Bn)]
+    check(lib, Bn, L, h, h_kv, 16 * rng.randint(1, 8), 16 * rng.randint(1, 8), P, own_max, lens, rng.randint(0, 1))
+
+
+@pytest.mark.parametrize("shape", [(64, 1, 8, 2, 64, 64, 9000, 512), (12, 5, 4, 4, 96, 128, 8191, 300), (32, 1, 4, 4, 32, 32, 4096, 500), (4, 1, 8, 2, 64, 64, 20000, 64),
+                                   (1, 1, 8, 2, 64, 64, 30000, 100), (40, 1, 4, 1, 128, 128, 3000, 700), (9, 2, 16, 2, 128, 96, 2500, 90), (24, 2, 4, 2, 32, 48, 1, 2000)])
+def test_long_prefixes_and_batches(lib, shape):
+    Bn, own_max = shape[0], shape[-1]
+    check(lib, *shape, [own_max - 31 * i % (own_max + 1) for i in range(Bn)], 1)
