@@ -103,8 +103,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_choose_kernel(const Evic
   __shared__ SelectShared sh;
   cache_choose(a, blockIdx.x, sh);
 }
-// Pieces `id`, id + step, .. of the kept rows of one cache, 16 bytes each, four at a time: row numbers, then rows, then stores, so that four rows of
+// Pieces `id`, id + step, .. of the kept rows of one cache, 16 bytes each, U at a time: row numbers, then rows, then stores, so that U rows of
 // a thread are on their way together.
+template <int U>
 __device__ __forceinline__ void cache_gather(const EvictArgs& a, int bh, int n, long long id0, long long most, int step) {
   const int b = bh / a.h_kv, hk = bh - b * a.h_kv, cq = a.kq >> 3, per = cq + (a.kv >> 3);
   const int* const idx = a.idx + static_cast<long long>(bh) * a.keep;
@@ -113,24 +114,24 @@ __device__ __forceinline__ void cache_gather(const EvictArgs& a, int bh, int n, 
   bf16_t* const ko = a.k_out + b * a.ko_sb + hk * a.ko_sh;
   bf16_t* const vo = a.v_out + b * a.vo_sb + hk * a.vo_sh;
   const long long all = static_cast<long long>(n) * per, end = all < most ? all : most;
-  for (long long id = id0; id < end; id += 4ll * step) {
-    int i[4], c[4], j[4];
-    uint4 x[4];
-    float w[4];
+  for (long long id = id0; id < end; id += static_cast<long long>(U) * step) {
+    int i[U], c[U], j[U];
+    uint4 x[U];
+    float w[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       const long long at = id + static_cast<long long>(u) * step < end ? id + static_cast<long long>(u) * step : id;
       i[u] = static_cast<int>(a.small ? __umulhi(static_cast<unsigned>(at), a.per_inv) : at / per);
       c[u] = static_cast<int>(at - static_cast<long long>(i[u]) * per);
       j[u] = min(max(idx[i[u]], 0), a.cap - 1);      // whatever a list holds, nothing outside the cache is read
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       x[u] = *reinterpret_cast<const uint4*>(c[u] < cq ? k + j[u] * a.k_st + c[u] * 8 : v + j[u] * a.v_st + (c[u] - cq) * 8);
       w[u] = c[u] == 0 && a.weights_out ? a.weights[static_cast<long long>(bh) * a.cap + j[u]] : 0.f;
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       if (id + static_cast<long long>(u) * step >= end) continue;
       *reinterpret_cast<uint4*>(c[u] < cq ? ko + i[u] * a.ko_st + c[u] * 8 : vo + i[u] * a.vo_st + (c[u] - cq) * 8) = x[u];
       if (c[u] == 0 && a.weights_out) a.weights_out[static_cast<long long>(bh) * a.cap_out + i[u]] = w[u];
@@ -140,7 +141,7 @@ __device__ __forceinline__ void cache_gather(const EvictArgs& a, int bh, int n, 
 __global__ __launch_bounds__(256) void cache_gather_kernel(const EvictArgs a) {
   const int bh = blockIdx.y, n = min(evict_len(a, bh / a.h_kv), a.keep);
   const long long first = static_cast<long long>(blockIdx.x) * 1024;
-  cache_gather(a, bh, n, first + threadIdx.x, first + 1024, 256);
+  cache_gather<4>(a, bh, n, first + threadIdx.x, first + 1024, 256);
 }
 // Both in one launch: the workgroup that chose the rows of a cache moves them.
 __global__ __launch_bounds__(SELECT_THREADS) void cache_evict_kernel(const EvictArgs a) {
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(SELECT_THREADS) void cache_evict_kernel(const Evict
   cache_choose(a, blockIdx.x, sh);
   __threadfence_block();
   __syncthreads();
-  cache_gather(a, blockIdx.x, min(evict_len(a, blockIdx.x / a.h_kv), a.keep), threadIdx.x, 1ll << 62, SELECT_THREADS);
+  cache_gather<2>(a, blockIdx.x, min(evict_len(a, blockIdx.x / a.h_kv), a.keep), threadIdx.x, 1ll << 62, SELECT_THREADS);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -8,15 +8,18 @@
 // matrix and every prefix key is read once for all of them; the own caches are read once each for the rows of their request.  Work is cut
 // into items (rows x range of keys, prefix or own); items of the same rows leave (m, l, O) in the workspace and a second launch joins them.
 //
-// Layout: scores are computed transposed on v_mfma_f32_16x16x32_bf16, S^T = K Q^T (16 keys x 16 rows): a row of the softmax is a lane's
-// column, and the four result registers of two key tiles are, rounded to bf16, the B operand of O^T = V^T P^T without going through LDS.
-// The matching V^T operand comes from transposing LDS reads.  Columns of 16 rather than 32: most calls have few rows (a token of a request
-// is g = h / h_kv rows), and the exponentials of unused columns are the largest cost beside the memory.
+// Layout: scores are computed transposed, S^T = K Q^T (keys x rows): a row of the softmax is a lane's column, and result registers are, rounded
+// to bf16, the B operand of O^T = V^T P^T without going through LDS.  The matching V^T operand comes from transposing LDS reads.  Few rows go
+// on v_mfma_f32_16x16x32_bf16, columns of 16 (Rows16): most calls have few (a token of a request is g = h / h_kv rows), and the exponentials of
+// unused columns are the largest cost beside the memory.  Many rows go on v_mfma_f32_32x32x16_bf16 (Rows32): half the matrix instructions and
+// half the steps of a maximum across lanes.
 //
 // Rounding: scores, maxima, sums and accumulators are fp32; the probabilities enter the second product rounded to bf16 (the matrix
 // unit's type), the denominator is summed from the unrounded ones, so that lse and the weights keep fp32 accuracy.
 #pragma once
 #include "attn_tile.h"
+
+#include <type_traits>
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
@@ -117,11 +120,22 @@ __device__ __forceinline__ float groups_sum(float v) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-// State of the NR x 16 rows of a wavefront.
-template <int DV, int NR>
-struct RowState {
+// The rows of a wavefront: queries, accumulators and running softmax.  m: running reference of raw scores, l: this lane's share of the sum of
+// exponentials (keys are spread over the lanes of a column).  chunk(c, q): four dims from dim(q) on of the row in column group c.
+//
+// The reference only has to keep the exponentials in range: it moves, and the accumulators are rescaled, when some row's maximum has grown by more
+// than RESCALE_LOG2 binades since it was set (at a row's first key: infinitely).
+template <int DQ, int DV, int NR>
+struct Rows16 {
+  static constexpr int COLS = NR, ROWS = 16 * NR, CHUNKS = DV / 16;
+  bf16x8_t qf[NR][DQ / 32];
   floatx4 o[NR][DV / 16];
-  float m[NR], l[NR];      // running reference of raw scores; this lane's share of the sum of exponentials
+  float m[NR], l[NR];
+  static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
+  static __device__ __forceinline__ int row(int c) { return 16 * c + (lane() & 15); }
+  static __device__ __forceinline__ int dim(int q) { return 16 * q + 4 * (lane() >> 4); }
+  static __device__ __forceinline__ bool lead() { return lane() < 16; }      // of the lanes of a column
+  __device__ __forceinline__ floatx4 chunk(int c, int q) const { return o[c][q]; }
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
@@ -131,116 +145,232 @@ struct RowState {
       for (int u = 0; u < DV / 16; ++u) o[c][u] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
   }
-};
-
-// One tile of KT keys.  left[c]: keys of this tile that the lane's row of column group c sees (any value: beyond KT all, below 1 none);
-// whole: every row sees all of the tile.  keep: where the scores of the lane's rows go (rows keep_pitch apart per column group; null: nowhere),
-// for the rows that `kept` has a bit for.
-template <int DQ, int DV, int NR, int KT>
-__device__ __forceinline__ void prefix_tile(const bf16_t* Kt, const bf16_t* Vt, const bf16x8_t (&qf)[NR][DQ / 32], RowState<DV, NR>& st, float sc,
-                                            bool whole, const int (&left)[NR], float* keep, int keep_pitch, unsigned kept) {
-  const int lane = threadIdx.x & 63, grp = lane >> 4, l16 = lane & 15;
-  floatx4 s[NR][KT / 16];
-  // Key fragments in groups of at most eight, all of a group read in front of its products, and products of the same 32 dims side by side: left
-  // to itself the compiler reads and waits for two fragments at a time and lets each product wait for the one before it.
-  constexpr int TG = KT / 16 < 8 / (DQ / 32) ? KT / 16 : 8 / (DQ / 32);
+  __device__ __forceinline__ void load(int c, const bf16_t* src, int kq, bool there) {
+    const int grp = lane() >> 4;
+    u32x4 raw[DQ / 32];
 #pragma unroll
-  for (int t0 = 0; t0 < KT / 16; t0 += TG) {
-    bf16x8_t kf[TG][DQ / 32];
+    for (int i = 0; i < DQ / 32; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + min(32 * i + 8 * grp, kq - 8));
 #pragma unroll
-    for (int t = 0; t < TG; ++t)
+    for (int i = 0; i < DQ / 32; ++i) qf[c][i] = __builtin_bit_cast(bf16x8_t, there && 32 * i + 8 * grp < kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
+  }
+  __device__ __forceinline__ void finish() {
 #pragma unroll
-      for (int i = 0; i < DQ / 32; ++i) kf[t][i] = *reinterpret_cast<const bf16x8_t*>(Kt + nat_off<DQ>(16 * (t0 + t) + l16, 4 * i + grp));
-    __builtin_amdgcn_sched_barrier(0);
+    for (int c = 0; c < NR; ++c) l[c] = groups_sum(l[c]);
+  }
+  // One tile of KT keys.  left[c]: keys of this tile that the lane's row of column group c sees (any value: beyond KT all, below 1 none);
+  // whole: every row sees all of the tile.  keep: where the scores of the lane's rows go (column groups 16 keep_pitch apart; null: nowhere),
+  // for the rows that `kept` has a bit for.
+  template <int KT>
+  __device__ __forceinline__ void tile(const bf16_t* Kt, const bf16_t* Vt, float sc, bool whole, const int (&left)[NR], float* keep, int keep_pitch, unsigned kept) {
+    const int grp = lane() >> 4, l16 = lane() & 15;
+    floatx4 s[NR][KT / 16];
+    // Key fragments in groups of at most eight, all of a group read in front of its products, and products of the same 32 dims side by side: left
+    // to itself the compiler reads and waits for two fragments at a time and lets each product wait for the one before it.
+    constexpr int TG = KT / 16 < 8 / (DQ / 32) ? KT / 16 : 8 / (DQ / 32);
 #pragma unroll
-    for (int i = 0; i < DQ / 32; ++i)
+    for (int t0 = 0; t0 < KT / 16; t0 += TG) {
+      bf16x8_t kf[TG][DQ / 32];
 #pragma unroll
       for (int t = 0; t < TG; ++t)
 #pragma unroll
-        for (int c = 0; c < NR; ++c)
-          s[c][t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][i], qf[c][i], i == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[c][t0 + t], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  if (!whole) {
+        for (int i = 0; i < DQ / 32; ++i) kf[t][i] = *reinterpret_cast<const bf16x8_t*>(Kt + nat_off<DQ>(16 * (t0 + t) + l16, 4 * i + grp));
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < NR; ++c)
+      for (int i = 0; i < DQ / 32; ++i)
+#pragma unroll
+        for (int t = 0; t < TG; ++t)
+#pragma unroll
+          for (int c = 0; c < NR; ++c)
+            s[c][t0 + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][i], qf[c][i], i == 0 ? floatx4{0.f, 0.f, 0.f, 0.f} : s[c][t0 + t], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int c = 0; c < NR; ++c)
+#pragma unroll
+        for (int t = 0; t < KT / 16; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[c][t][r] = 16 * t + 4 * grp + r < left[c] ? s[c][t][r] : -INFINITY;
+    }
+    if (keep) {
+#pragma unroll
+      for (int c = 0; c < NR; ++c)
+        if ((kept >> c) & 1u) {
+#pragma unroll
+          for (int t = 0; t < KT / 16; ++t) {
+            floatx4 x;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = s[c][t][r] * sc;
+            *reinterpret_cast<floatx4*>(keep + static_cast<long long>(c) * 16 * keep_pitch + 16 * t + 4 * grp) = x;
+          }
+        }
+    }
+    bool grown = false;
+    float m_new[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      float mx = s[c][0][0];
 #pragma unroll
       for (int t = 0; t < KT / 16; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[c][t][r] = 16 * t + 4 * grp + r < left[c] ? s[c][t][r] : -INFINITY;
-  }
-  if (keep) {
+        for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[c][t][r]);
+      m_new[c] = fmaxf(m[c], groups_max(mx));
+      grown |= (m_new[c] - m[c]) * sc > RESCALE_LOG2;
+    }
+    if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
 #pragma unroll
-    for (int c = 0; c < NR; ++c)
-      if ((kept >> c) & 1u) {
+      for (int c = 0; c < NR; ++c) {
+        const float alpha = m[c] == m_new[c] ? 1.f : __builtin_amdgcn_exp2f((m[c] - m_new[c]) * sc);
+        m[c] = m_new[c];
+        l[c] *= alpha;
 #pragma unroll
-        for (int t = 0; t < KT / 16; ++t) {
-          floatx4 x;
+        for (int u = 0; u < DV / 16; ++u)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) x[r] = s[c][t][r] * sc;
-          *reinterpret_cast<floatx4*>(keep + static_cast<long long>(c) * 16 * keep_pitch + 16 * t + 4 * grp) = x;
-        }
+          for (int r = 0; r < 4; ++r) o[c][u][r] *= alpha;
       }
-  }
-  // The reference only has to keep the exponentials in range: it moves, and the accumulators are rescaled, when some row's maximum has grown
-  // by more than RESCALE_LOG2 binades since it was set (or the row sees its first key).
-  bool grown = false;
-  float m_new[NR];
-#pragma unroll
-  for (int c = 0; c < NR; ++c) {
-    float mx = s[c][0][0];
-#pragma unroll
-    for (int t = 0; t < KT / 16; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[c][t][r]);
-    m_new[c] = fmaxf(st.m[c], groups_max(mx));
-    grown |= (m_new[c] - st.m[c]) * sc > RESCALE_LOG2;      // the first key: infinitely
-  }
-  if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
+    }
 #pragma unroll
     for (int c = 0; c < NR; ++c) {
-      const float alpha = st.m[c] == m_new[c] ? 1.f : __builtin_amdgcn_exp2f((st.m[c] - m_new[c]) * sc);
-      st.m[c] = m_new[c];
-      st.l[c] *= alpha;
+      const float msc = (m[c] == -INFINITY ? 0.f : m[c]) * sc;
 #pragma unroll
-      for (int u = 0; u < DV / 16; ++u)
+      for (int t = 0; t < KT / 16; ++t) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) st.o[c][u][r] *= alpha;
-    }
-  }
-#pragma unroll
-  for (int c = 0; c < NR; ++c) {
-    const float msc = (st.m[c] == -INFINITY ? 0.f : st.m[c]) * sc;
-    float sum = 0.f;
-#pragma unroll
-    for (int t = 0; t < KT / 16; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[c][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][t][r], sc, -msc));
-        sum += s[c][t][r];
+        for (int r = 0; r < 4; ++r) s[c][t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][t][r], sc, -msc));
+        l[c] += (s[c][t][0] + s[c][t][1]) + (s[c][t][2] + s[c][t][3]);
       }
-    st.l[c] += sum;
-  }
-#pragma unroll
-  for (int i = 0; i < KT / 32; ++i) {
-    TrnRegs vr[DV / 16];
-#pragma unroll
-    for (int u = 0; u < DV / 16; ++u) trn_issue16<DV>(vr[u], Vt, 16 * u, i);
-    bf16x8_t pf[NR];
-#pragma unroll
-    for (int c = 0; c < NR; ++c) {
-      const floatx8 p = {s[c][2 * i][0], s[c][2 * i][1], s[c][2 * i][2], s[c][2 * i][3], s[c][2 * i + 1][0], s[c][2 * i + 1][1], s[c][2 * i + 1][2], s[c][2 * i + 1][3]};
-      pf[c] = __builtin_convertvector(p, bf16x8_t);
     }
-    trn_wait();
 #pragma unroll
-    for (int u = 0; u < DV / 16; ++u) {
-      const bf16x8_t vf = trn_frag(vr[u]);
+    for (int i = 0; i < KT / 32; ++i) {
+      TrnRegs vr[DV / 16];
 #pragma unroll
-      for (int c = 0; c < NR; ++c) st.o[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], st.o[c][u], 0, 0, 0);
+      for (int u = 0; u < DV / 16; ++u) trn_issue16<DV>(vr[u], Vt, 16 * u, i);
+      bf16x8_t pf[NR];
+#pragma unroll
+      for (int c = 0; c < NR; ++c) {
+        const floatx8 p = {s[c][2 * i][0], s[c][2 * i][1], s[c][2 * i][2], s[c][2 * i][3], s[c][2 * i + 1][0], s[c][2 * i + 1][1], s[c][2 * i + 1][2], s[c][2 * i + 1][3]};
+        pf[c] = __builtin_convertvector(p, bf16x8_t);
+      }
+      trn_wait();
+#pragma unroll
+      for (int u = 0; u < DV / 16; ++u) {
+        const bf16x8_t vf = trn_frag(vr[u]);
+#pragma unroll
+        for (int c = 0; c < NR; ++c) o[c][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[c], o[c][u], 0, 0, 0);
+      }
     }
   }
-}
+};
+template <int DQ, int DV>
+struct Rows32 {
+  static constexpr int COLS = 1, ROWS = 32, CHUNKS = DV / 8;
+  bf16x8_t qf[DQ / 16];
+  floatx16 o[DV / 32];
+  float m[1], l[1];
+  static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
+  static __device__ __forceinline__ int row(int) { return lane() & 31; }
+  static __device__ __forceinline__ int dim(int q) { return 8 * q + 4 * (lane() >> 5); }
+  static __device__ __forceinline__ bool lead() { return lane() < 32; }
+  __device__ __forceinline__ floatx4 chunk(int, int q) const {
+    const floatx16& x = o[q >> 2];
+    return floatx4{x[4 * (q & 3)], x[4 * (q & 3) + 1], x[4 * (q & 3) + 2], x[4 * (q & 3) + 3]};
+  }
+  __device__ __forceinline__ void init() {
+    m[0] = -INFINITY;
+    l[0] = 0.f;
+#pragma unroll
+    for (int u = 0; u < DV / 32; ++u)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
+  }
+  __device__ __forceinline__ void load(int, const bf16_t* src, int kq, bool there) {
+    const int hh = lane() >> 5;
+    u32x4 raw[DQ / 16];
+#pragma unroll
+    for (int i = 0; i < DQ / 16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + min(16 * i + 8 * hh, kq - 8));
+#pragma unroll
+    for (int i = 0; i < DQ / 16; ++i) qf[i] = __builtin_bit_cast(bf16x8_t, there && 16 * i + 8 * hh < kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
+  }
+  __device__ __forceinline__ void finish() {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[0]), __float_as_uint(l[0]), false, false);
+    l[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  template <int KT>
+  __device__ __forceinline__ void tile(const bf16_t* Kt, const bf16_t* Vt, float sc, bool whole, const int (&left)[1], float*, int, unsigned) {
+    const int hh = lane() >> 5, l32 = lane() & 31;
+    floatx16 s[KT / 32];
+    constexpr int IG = DQ / 16 < 4 ? DQ / 16 : 4;      // 16 dims each: eight fragments of both key tiles in front of their products
+#pragma unroll
+    for (int i0 = 0; i0 < DQ / 16; i0 += IG) {
+      bf16x8_t kf[KT / 32][IG];
+#pragma unroll
+      for (int i = 0; i < IG; ++i)
+#pragma unroll
+        for (int t = 0; t < KT / 32; ++t) kf[t][i] = *reinterpret_cast<const bf16x8_t*>(Kt + nat_off<DQ>(32 * t + l32, 2 * (i0 + i) + hh));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < IG; ++i)
+#pragma unroll
+        for (int t = 0; t < KT / 32; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t][i], qf[i0 + i], i0 + i == 0 ? floatx16{} : s[t], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < left[0] ? s[t][r] : -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
+    {
+      const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    const float m_new = fmaxf(m[0], mx);
+    if (__builtin_amdgcn_ballot_w64((m_new - m[0]) * sc > RESCALE_LOG2) != 0ull) {
+      const float alpha = m[0] == m_new ? 1.f : __builtin_amdgcn_exp2f((m[0] - m_new) * sc);
+      m[0] = m_new;
+      l[0] *= alpha;
+#pragma unroll
+      for (int u = 0; u < DV / 32; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[u][r] *= alpha;
+    }
+    const float msc = (m[0] == -INFINITY ? 0.f : m[0]) * sc;
+#pragma unroll
+    for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r + e], sc, -msc));
+        l[0] += (s[t][r] + s[t][r + 1]) + (s[t][r + 2] + s[t][r + 3]);
+      }
+#pragma unroll
+    for (int i = 0; i < KT / 32; ++i) {      // 32 keys: two products a block of dims
+      TrnRegs vr[2][DV / 32];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int u = 0; u < DV / 32; ++u) trn_issue<DV>(vr[e][u], Vt, 32 * u, 2 * i + e);
+      bf16x8_t pf[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        floatx8 p;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p[r] = s[i][8 * e + r];
+        pf[e] = __builtin_convertvector(p, bf16x8_t);
+      }
+      trn_wait();
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int u = 0; u < DV / 32; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trn_frag(vr[e][u]), pf[e], o[u], 0, 0, 0);
+    }
+  }
+};
 
 // What an item is.
 struct Item {
@@ -313,23 +443,30 @@ __device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, 
   }
 }
 
-// Key tiles of an item, stages of LDS buffers and their bytes.  Shared tiles have 64 keys; a wavefront's own ones 32, so that two stages for four
-// wavefronts take as much as four stages of shared tiles.
-template <int DQ, int DV, int NR, bool SHARE, int NB>
+// Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64 or 128, 16 or 32 a wavefront, and every tile shared.
+enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3 };
+// Key tiles, LDS buffers of NB stages and their bytes.  Shared tiles have 64 keys; a wavefront's own ones 32, so that two stages for four wavefronts take
+// as much as four stages of shared tiles.
+template <int DQ, int DV, int ROWS, int NB>
 struct PrefixShape {
-  static constexpr int KT = SHARE ? 64 : 32;
-  static constexpr int loop = (SHARE ? 1 : 4) * NB * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * NR * (DV * 16 + 32) + NR * 16) * 4;
+  static constexpr bool SHARE = ROWS >= ROWS_64;
+  typedef std::conditional_t<ROWS == ROWS_128, Rows32<DQ, DV>, Rows16<DQ, DV, ROWS == ROWS_32 ? 2 : 1>> Rows;
+  static constexpr int KT = SHARE ? 64 : 32, ROW_TILE = 16 << ROWS;
+  static constexpr int loop = (SHARE ? 1 : 4) * NB * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * Rows::COLS * (DV * 16 + 32) + Rows::COLS * 16) * 4;
   static constexpr int lds = loop > join ? loop : join;
 };
 
-// SHARE: the four wavefronts take NR * 16 rows each and share every key tile.  Otherwise they share the item's rows (at most NR * 16) and take
-// the key tiles in turn, from LDS buffers of their own without a barrier, and join at the end.  NB stages: NB - 1 tiles are on their way.
-template <int DQ, int DV, int NR, bool SHARE, int NB>
+// An item.  Shared tiles: the four wavefronts take their rows each.  Otherwise they share the item's rows and take the key tiles in turn, from
+// LDS buffers of their own without a barrier, and join at the end.  NB stages: NB - 1 tiles are on their way.
+template <int DQ, int DV, int ROWS, int NB>
 __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const lds_all) {
-  constexpr int KT = PrefixShape<DQ, DV, NR, SHARE, NB>::KT, WAVES = SHARE ? 4 : 1;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4, l16 = lane & 15;
+  typedef PrefixShape<DQ, DV, ROWS, NB> Shape;
+  typedef typename Shape::Rows Rows;
+  constexpr bool SHARE = Shape::SHARE;
+  constexpr int KT = Shape::KT, WAVES = SHARE ? 4 : 1, COLS = Rows::COLS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Item it;
-  if (!prefix_item<KT>(a, (SHARE ? 4 : 1) * NR * 16, it)) return;
+  if (!prefix_item<KT>(a, Shape::ROW_TILE, it)) return;
   bf16_t* const buf = lds_all + (SHARE ? 0 : wave * NB * KT * (DQ + DV));      // [NB][K tile, V tile]
 
   KvLoader<DQ, KT, WAVES> kl;
@@ -356,126 +493,121 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
     if (first + i * STEP < it.t1) issue(first + i * STEP, i);
 
   // the wavefront's rows: queries straight from memory, rows and dims outside are zero
-  bf16x8_t qf[NR][DQ / 32];
-  int seen[NR];      // own keys the row sees
+  Rows st;
+  st.init();
+  const int first_row = SHARE ? wave * Rows::ROWS : 0;
+  const bool idle = first_row >= it.n_rows;      // a wavefront without rows only loads
+  int seen[COLS];                                // own keys the row sees
+  unsigned kept = 0u;
 #pragma unroll
-  for (int c = 0; c < NR; ++c) {
-    const int r = (SHARE ? wave * NR * 16 : 0) + c * 16 + l16, row = it.row0 + min(r, it.n_rows - 1);
-    const int token = row / a.g;
-    const bf16_t* const src = a.q + token * a.ld_q + static_cast<long long>(it.hk * a.g + (row - token * a.g)) * a.kq;
+  for (int c = 0; c < COLS; ++c) {
+    const int r = first_row + Rows::row(c), row = it.row0 + min(r, it.n_rows - 1), token = row / a.g;
+    st.load(c, a.q + token * a.ld_q + static_cast<long long>(it.hk * a.g + (row - token * a.g)) * a.kq, a.kq, r < it.n_rows);
     seen[c] = it.b < 0 ? 0 : own_visible(own_len(a, it.b), a.L, token - it.b * a.L);
-    u32x4 raw[DQ / 32];
-#pragma unroll
-    for (int i = 0; i < DQ / 32; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + min(32 * i + 8 * grp, a.kq - 8));
-#pragma unroll
-    for (int i = 0; i < DQ / 32; ++i)
-      qf[c][i] = __builtin_bit_cast(bf16x8_t, r < it.n_rows && 32 * i + 8 * grp < a.kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
+    kept |= r < it.n_rows ? 1u << c : 0u;
   }
   int least = seen[0];
 #pragma unroll
-  for (int c = 1; c < NR; ++c) least = min(least, seen[c]);
+  for (int c = 1; c < COLS; ++c) least = min(least, seen[c]);
   least = static_cast<int>(wave_umin(static_cast<uint32_t>(least)));      // own keys that every row sees
-
   // scores of own keys are kept where the call wants weights (then an item has all rows of its request)
-  const int first_row = SHARE ? wave * NR * 16 : 0;
-  const bool idle = first_row >= it.n_rows;      // a wavefront without rows only loads
-  float* const keep = a.scores && it.b >= 0 ? a.scores + (static_cast<long long>(it.b * a.h_kv + it.hk) * a.own_rows + first_row + l16) * a.own_pad : nullptr;
-  unsigned kept = 0u;
-#pragma unroll
-  for (int c = 0; c < NR; ++c) kept |= first_row + c * 16 + l16 < it.n_rows ? 1u << c : 0u;
+  float* const keep = a.scores && it.b >= 0 ? a.scores + (static_cast<long long>(it.b * a.h_kv + it.hk) * a.own_rows + first_row + Rows::row(0)) * a.own_pad : nullptr;
 
-  RowState<DV, NR> st;
-  st.init();
-  int cur = 0;
-  for (int j = first; j < it.t1; j += STEP) {
-    // of the operations issued since this tile's loads, at least those of the NB - 2 tiles behind it are loads that may still be under way
-    if (NB > 2 && j + (NB - 2) * STEP < it.t1) loads_wait<(NB - 2) * (KvLoader<DQ, KT, WAVES>::PER + KvLoader<DV, KT, WAVES>::PER)>();
-    else stream_wait();
-    if (SHARE) __syncthreads();
-    if (j + (NB - 1) * STEP < it.t1) issue(j + (NB - 1) * STEP, cur == 0 ? NB - 1 : cur - 1);
-    cur = cur + 1 == NB ? 0 : cur + 1;
-    if (idle) continue;
-    const bool own = j >= it.split;
-    const int k0 = (own ? j - it.split : j) * KT;
-    int left[NR];
+  int j = first;
+  while (j < it.t1) {
 #pragma unroll
-    for (int c = 0; c < NR; ++c) left[c] = (own ? seen[c] : a.P) - k0;
-    const bf16_t* const at = buf + (cur == 0 ? NB - 1 : cur - 1) * (KT * (DQ + DV));
-    prefix_tile<DQ, DV, NR, KT>(at, at + KT * DQ, qf, st, a.sc, k0 + KT <= (own ? least : a.P), left, own && keep ? keep + k0 : nullptr, a.own_pad, kept);
+    for (int n = 0; n < NB; ++n) {      // a stage's buffer is known to the compiler
+      if (j >= it.t1) break;
+      // of the operations issued since this tile's loads, at least those of the NB - 2 tiles behind it are loads that may still be under way
+      if (NB > 2 && j + (NB - 2) * STEP < it.t1) loads_wait<(NB - 2) * (KvLoader<DQ, KT, WAVES>::PER + KvLoader<DV, KT, WAVES>::PER)>();
+      else stream_wait();
+      if (SHARE) __syncthreads();
+      if (j + (NB - 1) * STEP < it.t1) issue(j + (NB - 1) * STEP, (n + NB - 1) % NB);
+      if (!idle) {
+        const bool own = j >= it.split;
+        const int k0 = (own ? j - it.split : j) * KT;
+        int left[COLS];
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) left[c] = (own ? seen[c] : a.P) - k0;
+        const bf16_t* const at = buf + n * (KT * (DQ + DV));
+        st.template tile<KT>(at, at + KT * DQ, a.sc, k0 + KT <= (own ? least : a.P), left, own && keep ? keep + k0 : nullptr, a.own_pad, kept);
+      }
+      j += STEP;
+    }
   }
-#pragma unroll
-  for (int c = 0; c < NR; ++c) st.l[c] = groups_sum(st.l[c]);
+  st.finish();
 
-  // this lane's four dims of block u of row r: normalised into the output, or a piece for the join
-  const auto write = [&](int c, int u, const floatx4& acc, float m, float l, bool with_ml) __attribute__((always_inline)) {
-    const int r = (SHARE ? wave * NR * 16 : 0) + c * 16 + l16, row = it.row0 + r;
+  // this lane's four dims of chunk q of its row: normalised into the output, or a piece for the join
+  const auto write = [&](int c, int q, const floatx4& acc, float m, float l) __attribute__((always_inline)) {
+    const int r = first_row + Rows::row(c), row = it.row0 + r, d = Rows::dim(q);
     if (r >= it.n_rows) return;
     if (a.slots == 0) {
       const int token = row / a.g, head = it.hk * a.g + (row - token * a.g);
-      if (16 * u < a.kv) {
+      if (d < a.kv) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
         floatx4 f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = acc[i] * inv;
-        *reinterpret_cast<bf16x4_t*>(a.o + token * a.ld_o + static_cast<long long>(head) * a.kv + 16 * u + 4 * grp) = __builtin_convertvector(f, bf16x4_t);
+        *reinterpret_cast<bf16x4_t*>(a.o + token * a.ld_o + static_cast<long long>(head) * a.kv + d) = __builtin_convertvector(f, bf16x4_t);
       }
-      if (with_ml && a.lse && grp == 0) {
+      if (q == 0 && a.lse && Rows::lead()) {
         const int b = token / a.L;
         a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l > 0.f ? (m * a.sc + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
       }
     } else {
       const long long at = (static_cast<long long>(it.hk) * a.rows + row) * a.slots + it.slot;
-      if (16 * u < a.kv) *reinterpret_cast<floatx4*>(a.part_o + at * a.kv + 16 * u + 4 * grp) = acc;
-      if (with_ml && grp == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m * a.sc, l};
+      if (d < a.kv) *reinterpret_cast<floatx4*>(a.part_o + at * a.kv + d) = acc;
+      if (q == 0 && Rows::lead()) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = float2{m * a.sc, l};
     }
   };
-  if (SHARE) {
+  if constexpr (SHARE) {
 #pragma unroll
-    for (int c = 0; c < NR; ++c)
+    for (int c = 0; c < COLS; ++c)
 #pragma unroll
-      for (int u = 0; u < DV / 16; ++u) write(c, u, st.o[c][u], st.m[c], st.l[c], u == 0);
+      for (int q = 0; q < Rows::CHUNKS; ++q) write(c, q, st.chunk(c, q), st.m[c], st.l[c]);
   } else {
+    constexpr int U = DV / 16;
     __syncthreads();
-    float* const part = reinterpret_cast<float*>(lds_all);      // [4][NR][DV / 16][4][64]
-    float* const ms = part + 4 * NR * DV * 16;                  // [4][NR][16] each
-    float* const ls = ms + 4 * NR * 16;
-    float* const lse2 = ls + 4 * NR * 16;                       // [NR][16]
+    float* const part = reinterpret_cast<float*>(lds_all);       // [4][COLS][U][64][4]
+    float* const ms = part + 4 * COLS * DV * 16;                 // [4][COLS][16] each
+    float* const ls = ms + 4 * COLS * 16;
+    float* const lse2 = ls + 4 * COLS * 16;                      // [COLS][16]
+    const int l16 = lane & 15;
 #pragma unroll
-    for (int c = 0; c < NR; ++c) {
+    for (int c = 0; c < COLS; ++c) {
 #pragma unroll
-      for (int u = 0; u < DV / 16; ++u)
-        *reinterpret_cast<floatx4*>(part + (((wave * NR + c) * (DV / 16) + u) * 64 + lane) * 4) = st.o[c][u];
-      if (grp == 0) {
-        ms[(wave * NR + c) * 16 + l16] = st.m[c];
-        ls[(wave * NR + c) * 16 + l16] = st.l[c];
+      for (int u = 0; u < U; ++u) *reinterpret_cast<floatx4*>(part + (((wave * COLS + c) * U + u) * 64 + lane) * 4) = st.chunk(c, u);
+      if (Rows::lead()) {
+        ms[(wave * COLS + c) * 16 + l16] = st.m[c];
+        ls[(wave * COLS + c) * 16 + l16] = st.l[c];
       }
     }
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < NR; ++c) {
+    for (int c = 0; c < COLS; ++c) {
       float m_all = ms[c * 16 + l16], al[4], l_all = 0.f;
 #pragma unroll
-      for (int w = 1; w < 4; ++w) m_all = fmaxf(m_all, ms[(w * NR + c) * 16 + l16]);
+      for (int w = 1; w < 4; ++w) m_all = fmaxf(m_all, ms[(w * COLS + c) * 16 + l16]);
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const float m = ms[(w * NR + c) * 16 + l16];
+        const float m = ms[(w * COLS + c) * 16 + l16];
         al[w] = m == m_all ? (m == -INFINITY ? 0.f : 1.f) : __builtin_amdgcn_exp2f((m - m_all) * a.sc);
-        l_all += al[w] * ls[(w * NR + c) * 16 + l16];
+        l_all += al[w] * ls[(w * COLS + c) * 16 + l16];
       }
 #pragma unroll
-      for (int u0 = 0; u0 < DV / 16; u0 += 4) {
+      for (int u0 = 0; u0 < U; u0 += 4) {
         const int u = u0 + wave;
-        if (u >= DV / 16) break;
+        if (u >= U) break;
         floatx4 f = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const floatx4 x = *reinterpret_cast<const floatx4*>(part + (((w * NR + c) * (DV / 16) + u) * 64 + lane) * 4);
+          const floatx4 x = *reinterpret_cast<const floatx4*>(part + (((w * COLS + c) * U + u) * 64 + lane) * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[i] += al[w] * x[i];
         }
-        write(c, u, f, m_all, l_all, u == 0);
+        write(c, u, f, m_all, l_all);
       }
-      if (a.slots == 0 && wave == 0 && grp == 0) lse2[c * 16 + l16] = l_all > 0.f ? m_all * a.sc + __builtin_amdgcn_logf(l_all) : INFINITY;
+      if (a.slots == 0 && wave == 0 && Rows::lead()) lse2[c * 16 + l16] = l_all > 0.f ? m_all * a.sc + __builtin_amdgcn_logf(l_all) : INFINITY;
     }
     if (a.slots == 0 && keep) {      // the item has seen all of its rows' keys: weights from the scores it kept
       __threadfence_block();
@@ -486,19 +618,12 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
   }
 }
 
-// Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64 or 128, 16 or 32 a wavefront.
-enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3 };
-template <int DQ, int DV, int ROWS, int NB>
-__device__ __forceinline__ void prefix_kind(const PrefixArgs& a, bf16_t* lds) {
-  prefix_rows<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>(a, lds);
-}
 // OWN: rows of the items of a request; PREFIX: of those of the prefix alone, in front of them in the grid (the same: all items are of one kind).
 // Shared tiles have four stages beside own ones (whose LDS is there anyway), else few enough for several workgroups on a compute unit.
 template <int DQ, int DV, int OWN, int PREFIX>
 struct PrefixKernel {
   static constexpr int NB_S = DQ + DV <= 128 && OWN == ROWS_64 ? 3 : 2, NB_O = OWN >= ROWS_64 ? NB_S : 2, NB_P = PREFIX < ROWS_64 ? 2 : (OWN >= ROWS_64 ? NB_S : 4);
-  template <int ROWS, int NB> static constexpr int lds_of() { return PrefixShape<DQ, DV, ROWS == ROWS_16 || ROWS == ROWS_64 ? 1 : 2, (ROWS >= ROWS_64), NB>::lds; }
-  static constexpr int own = lds_of<OWN, NB_O>(), pre = OWN == PREFIX ? 0 : lds_of<PREFIX, NB_P>();
+  static constexpr int own = PrefixShape<DQ, DV, OWN, NB_O>::lds, pre = OWN == PREFIX ? 0 : PrefixShape<DQ, DV, PREFIX, NB_P>::lds;
   static constexpr int lds = own > pre ? own : pre;
 };
 // Two wavefronts a SIMD at least: the register file then has no accumulation half, and the scores need no moves between the halves.
@@ -506,13 +631,16 @@ template <int DQ, int DV, int OWN, int PREFIX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_attn_kernel(const PrefixArgs a) {
   typedef PrefixKernel<DQ, DV, OWN, PREFIX> K;
   extern __shared__ __attribute__((aligned(16))) bf16_t lds_all[];      // one object: see attn.hip
-  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_kind<DQ, DV, PREFIX, K::NB_P>(a, lds_all);
-  else prefix_kind<DQ, DV, OWN, K::NB_O>(a, lds_all);
+  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_rows<DQ, DV, PREFIX, K::NB_P>(a, lds_all);
+  else prefix_rows<DQ, DV, OWN, K::NB_O>(a, lds_all);
 }
 
-// the pairs that are built
-#define PREFIX_KINDS(X) X(ROWS_16, ROWS_16) X(ROWS_32, ROWS_32) X(ROWS_64, ROWS_64) X(ROWS_128, ROWS_128) X(ROWS_16, ROWS_32) \
-  X(ROWS_16, ROWS_64) X(ROWS_32, ROWS_64) X(ROWS_16, ROWS_128) X(ROWS_32, ROWS_128) X(ROWS_64, ROWS_128)
+// The pairs that are built: items of one kind for every width; apart, own tiles beside the prefix's for narrow heads, and shared ones for wide heads,
+// where own tiles of every wavefront would leave a compute unit one workgroup (prefix_plan()).
+#define PREFIX_KINDS_ALL(X, DQ, DV) X(DQ, DV, ROWS_16, ROWS_16) X(DQ, DV, ROWS_32, ROWS_32) X(DQ, DV, ROWS_64, ROWS_64) X(DQ, DV, ROWS_128, ROWS_128)
+#define PREFIX_KINDS_NARROW(X, DQ, DV) X(DQ, DV, ROWS_16, ROWS_32) X(DQ, DV, ROWS_16, ROWS_64) X(DQ, DV, ROWS_32, ROWS_64) X(DQ, DV, ROWS_16, ROWS_128) X(DQ, DV, ROWS_32, ROWS_128)
+#define PREFIX_KINDS_WIDE(X, DQ, DV) X(DQ, DV, ROWS_64, ROWS_128)
+constexpr bool prefix_wide(int dq, int dv) { return dq + dv > 128; }
 template <int DQ, int DV, int OWN, int PREFIX>
 static hipError_t prefix_launch(const PrefixArgs& a, unsigned grid, hipStream_t st) {
   constexpr int lds = PrefixKernel<DQ, DV, OWN, PREFIX>::lds;
@@ -527,8 +655,13 @@ static hipError_t prefix_launch(const PrefixArgs& a, unsigned grid, hipStream_t 
 }
 template <int DQ, int DV>
 static hipError_t prefix_launch_width(const PrefixArgs& a, int own, int prefix, unsigned grid, hipStream_t st) {
-#define PREFIX_KIND(O, P) if (own == O && prefix == P) return prefix_launch<DQ, DV, O, P>(a, grid, st);
-  PREFIX_KINDS(PREFIX_KIND)
+#define PREFIX_KIND(Q, V, O, P) if (own == O && prefix == P) return prefix_launch<Q, V, O, P>(a, grid, st);
+  PREFIX_KINDS_ALL(PREFIX_KIND, DQ, DV)
+  if constexpr (prefix_wide(DQ, DV)) {
+    PREFIX_KINDS_WIDE(PREFIX_KIND, DQ, DV)
+  } else {
+    PREFIX_KINDS_NARROW(PREFIX_KIND, DQ, DV)
+  }
 #undef PREFIX_KIND
   return hipErrorInvalidValue;
 }

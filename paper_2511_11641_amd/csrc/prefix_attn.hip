@@ -274,7 +274,7 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   const bool only_joint = a.B == 1 || a.P == 0 || p.own >= ROWS_64;
   // Wide heads apart: own tiles for every wavefront take so much LDS that one workgroup is left to a compute unit; shared tiles leave two, and a
   // wavefront with the few rows keeps up with memory (12 x 5 tokens on 8191, 96 and 128 dims: 49 -> 44 us; 64 and 64 dims: no difference).
-  const int own = p.own, apart_own = p.dq + p.dv > 128 ? ROWS_64 : p.own;
+  const int own = p.own, apart_own = prefix_wide(p.dq, p.dv) ? ROWS_64 : p.own;
   const double joint = only_joint ? 0 : plan_joint(a, p, resident_joint, false);
   p.own = apart_own;
   if (!only_joint && plan_apart(a, p, apart_own == ROWS_64 ? resident_128 : resident_own, false) < joint) {

@@ -2,11 +2,10 @@
 #include "prefix_attn.h"
 
 // explicit instantiation: left to the launch code, the host side of this compiler can drop some of the kernel stubs
-#define PREFIX_INSTANTIATE(O, P)                                                     \
-  template __global__ void prefix_attn_kernel<128, 32, O, P>(const PrefixArgs);  \
-  template __global__ void prefix_attn_kernel<128, 64, O, P>(const PrefixArgs);  \
-  template __global__ void prefix_attn_kernel<128, 128, O, P>(const PrefixArgs);
-PREFIX_KINDS(PREFIX_INSTANTIATE)
+#define PREFIX_INSTANTIATE(Q, V, O, P) template __global__ void prefix_attn_kernel<Q, V, O, P>(const PrefixArgs);
+PREFIX_KINDS_ALL(PREFIX_INSTANTIATE, 128, 32) PREFIX_KINDS_WIDE(PREFIX_INSTANTIATE, 128, 32)
+PREFIX_KINDS_ALL(PREFIX_INSTANTIATE, 128, 64) PREFIX_KINDS_WIDE(PREFIX_INSTANTIATE, 128, 64)
+PREFIX_KINDS_ALL(PREFIX_INSTANTIATE, 128, 128) PREFIX_KINDS_WIDE(PREFIX_INSTANTIATE, 128, 128)
 #undef PREFIX_INSTANTIATE
 
 hipError_t prefix_launch_128(const PrefixArgs& a, int dv, int own, int prefix, unsigned grid, hipStream_t st) {

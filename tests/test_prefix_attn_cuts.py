@@ -10,7 +10,7 @@ from paper_2511_11641_amd import binding as B
 
 FIELDS = ("joint", "p_tiles", "p_chunks", "p_chunk", "p_row_tiles", "p_items", "o_chunks", "o_chunk", "o_row_tiles", "slots", "own", "prefix", "grid", "weigh", "own_pad", "keep")
 ROWS, KEYS, AT_ONCE = (16, 32, 64, 128), (32, 32, 64, 64), (4, 4, 1, 1)
-PAIRS = {(0, 0), (1, 1), (2, 2), (3, 3), (0, 1), (0, 2), (1, 2), (0, 3), (1, 3), (2, 3)}      # the kernels that are built
+SAME, NARROW, WIDE = {(0, 0), (1, 1), (2, 2), (3, 3)}, {(0, 1), (0, 2), (1, 2), (0, 3), (1, 3)}, {(2, 3)}      # the kernels that are built
 
 
 def cut(lib, Bn, L, h, h_kv, e, f, P, own_max, weights=1):
@@ -53,7 +53,8 @@ def check(lib, Bn, L, h, h_kv, e, f, P, own_max, lens, weights):
     a["own_max"] = own_max
     g = h // h_kv
     own_rows, rows = L * g, Bn * L * g
-    assert (a["own"], a["prefix"]) in PAIRS and a["p_tiles"] == -(-P // KEYS[a["prefix"]])
+    width = lambda n: 32 if n <= 32 else (64 if n <= 64 else 128)
+    assert (a["own"], a["prefix"]) in SAME | (WIDE if width(e) + width(f) > 128 else NARROW) and a["p_tiles"] == -(-P // KEYS[a["prefix"]])
     assert ROWS[a["own"]] >= min(own_rows, 128) and a["o_row_tiles"] == -(-own_rows // ROWS[a["own"]])
     assert a["own_pad"] >= -(-own_max // KEYS[a["own"]]) * KEYS[a["own"]] and a["own_pad"] % 4 == 0
     if a["keep"]:
