@@ -421,26 +421,30 @@ __device__ __forceinline__ PrefixScores prefix_scores(const PrefixArgs& a, long 
   for (int i = 0; i < 4; ++i) s.x[i] = *reinterpret_cast<const floatx4*>(scores + static_cast<long long>(min(r0 + i, a.own_rows - 1)) * a.own_pad);
   return s;
 }
-// Accumulated weights of own keys j0 .. j0 + 3, j0 + step .. of request and head bh, from the kept scores of its rows: w_out = w_in + sum over the
-// rows of exp2(score - lse2).  early: prefix_scores() of rows 0 .. 3 and key j0.
-__device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, PrefixScores early, const float* lse2, int n, int j0, int step) {
-  for (int j = j0; j < n; j += step) {
-    float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
+__device__ __forceinline__ floatx4 prefix_weights_before(const PrefixArgs& a, long long bh, int j, int n) {
+  floatx4 w = {0.f, 0.f, 0.f, 0.f};
+  if (a.w_in) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) was[e] = a.w_in ? a.w_in[bh * a.cap + min(j + e, n - 1)] : 0.f;
-    for (int r = 0; r < a.own_rows; r += 4) {
-      const PrefixScores s = r == 0 && j == j0 ? early : prefix_scores(a, bh, r, j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float ref = r + i < a.own_rows ? lse2[r + i] : INFINITY;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(s.x[i][e] - ref);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e < n) a.w_out[bh * a.cap + j + e] = was[e] + sum[e];
+    for (int e = 0; e < 4; ++e) w[e] = a.w_in[bh * a.cap + min(j + e, n - 1)];
   }
+  return w;
+}
+// Accumulated weights of own keys j .. j + 3 (those below n) of request and head bh, from the kept scores of its rows: w_out = w_in + sum over the rows of
+// exp2(score - lse2).  early: prefix_scores() of rows 0 .. 3, before: prefix_weights_before(), both asked for in front of what lse2 waits for.
+__device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, PrefixScores early, const floatx4& before, const float* lse2, int n, int j) {
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < a.own_rows; r += 4) {
+    if (r > 0) early = prefix_scores(a, bh, r, j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float ref = r + i < a.own_rows ? lse2[r + i] : INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(early.x[i][e] - ref);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < n) a.w_out[bh * a.cap + j + e] = before[e] + sum[e];
 }
 
 // Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64 or 128, 16 or 32 a wavefront, and every tile shared.
@@ -613,7 +617,8 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
       __threadfence_block();
       __syncthreads();
       const long long bh = static_cast<long long>(it.b) * a.h_kv + it.hk;
-      if (it.own_n > 0) prefix_weigh(a, bh, prefix_scores(a, bh, 0, min(static_cast<int>(threadIdx.x) * 4, a.own_pad - 4)), lse2, it.own_n, threadIdx.x * 4, 1024);
+      for (int k = threadIdx.x * 4; k < it.own_n; k += 1024)
+        prefix_weigh(a, bh, prefix_scores(a, bh, 0, k), prefix_weights_before(a, bh, k, it.own_n), lse2, it.own_n, k);
     }
   }
 }

@@ -23,7 +23,9 @@ __device__ void prefix_join_weights(const PrefixArgs& a, int kt, int row_tile, l
   const int bh = static_cast<int>(id / per), b = bh / a.h_kv, hk = bh - b * a.h_kv, first = static_cast<int>(id - static_cast<long long>(bh) * per) * 1024;
   const int n = own_len(a, b), lane = threadIdx.x & 63;
   if (first >= n) return;
-  const PrefixScores early = prefix_scores(a, bh, 0, min(first + static_cast<int>(threadIdx.x) * 4, a.own_pad - 4));
+  const int key = first + static_cast<int>(threadIdx.x) * 4;
+  const PrefixScores early = prefix_scores(a, bh, 0, min(key, a.own_pad - 4));
+  const floatx4 before = prefix_weights_before(a, bh, key, n);
   for (int r = threadIdx.x >> 6; r < a.own_rows; r += 4) {
     const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) + (static_cast<long long>(hk) * a.rows + b * a.own_rows + r) * a.slots;
     const int pieces = prefix_pieces(a, b, r, kt, row_tile);
@@ -39,7 +41,7 @@ __device__ void prefix_join_weights(const PrefixArgs& a, int kt, int row_tile, l
     if (lane == 0) lse2[r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
   }
   __syncthreads();
-  prefix_weigh(a, bh, early, lse2, min(n, first + 1024), first + threadIdx.x * 4, 1024);
+  if (key < n) prefix_weigh(a, bh, early, before, lse2, n, key);
 }
 template <int W, bool FEW>      // threads of a piece: kp_vo / 4 rounded up to a power of two
 __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, int kt, int row_tile, unsigned row_blocks) {
