@@ -260,44 +260,50 @@ struct Rows16 {
     }
   }
 };
-template <int DQ, int DV>
+template <int DQ, int DV, int NR>
 struct Rows32 {
-  static constexpr int COLS = 1, ROWS = 32, CHUNKS = DV / 8;
-  bf16x8_t qf[DQ / 16];
-  floatx16 o[DV / 32];
-  float m[1], l[1];
+  static constexpr int COLS = NR, ROWS = 32 * NR, CHUNKS = DV / 8;
+  bf16x8_t qf[NR][DQ / 16];
+  floatx16 o[NR][DV / 32];
+  float m[NR], l[NR];
   static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
-  static __device__ __forceinline__ int row(int) { return lane() & 31; }
+  static __device__ __forceinline__ int row(int c) { return 32 * c + (lane() & 31); }
   static __device__ __forceinline__ int dim(int q) { return 8 * q + 4 * (lane() >> 5); }
   static __device__ __forceinline__ bool lead() { return lane() < 32; }
-  __device__ __forceinline__ floatx4 chunk(int, int q) const {
-    const floatx16& x = o[q >> 2];
+  __device__ __forceinline__ floatx4 chunk(int c, int q) const {
+    const floatx16& x = o[c][q >> 2];
     return floatx4{x[4 * (q & 3)], x[4 * (q & 3) + 1], x[4 * (q & 3) + 2], x[4 * (q & 3) + 3]};
   }
   __device__ __forceinline__ void init() {
-    m[0] = -INFINITY;
-    l[0] = 0.f;
 #pragma unroll
-    for (int u = 0; u < DV / 32; ++u)
+    for (int c = 0; c < NR; ++c) {
+      m[c] = -INFINITY;
+      l[c] = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[u][r] = 0.f;
+      for (int u = 0; u < DV / 32; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][u][r] = 0.f;
+    }
   }
-  __device__ __forceinline__ void load(int, const bf16_t* src, int kq, bool there) {
+  __device__ __forceinline__ void load(int c, const bf16_t* src, int kq, bool there) {
     const int hh = lane() >> 5;
     u32x4 raw[DQ / 16];
 #pragma unroll
     for (int i = 0; i < DQ / 16; ++i) raw[i] = *reinterpret_cast<const u32x4*>(src + min(16 * i + 8 * hh, kq - 8));
 #pragma unroll
-    for (int i = 0; i < DQ / 16; ++i) qf[i] = __builtin_bit_cast(bf16x8_t, there && 16 * i + 8 * hh < kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
+    for (int i = 0; i < DQ / 16; ++i) qf[c][i] = __builtin_bit_cast(bf16x8_t, there && 16 * i + 8 * hh < kq ? raw[i] : u32x4{0u, 0u, 0u, 0u});
   }
   __device__ __forceinline__ void finish() {
-    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[0]), __float_as_uint(l[0]), false, false);
-    l[0] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[c]), __float_as_uint(l[c]), false, false);
+      l[c] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
   }
   template <int KT>
-  __device__ __forceinline__ void tile(const bf16_t* Kt, const bf16_t* Vt, float sc, bool whole, const int (&left)[1], float*, int, unsigned) {
+  __device__ __forceinline__ void tile(const bf16_t* Kt, const bf16_t* Vt, float sc, bool whole, const int (&left)[NR], float*, int, unsigned) {
     const int hh = lane() >> 5, l32 = lane() & 31;
-    floatx16 s[KT / 32];
+    floatx16 s[NR][KT / 32];
     constexpr int IG = DQ / 16 < 4 ? DQ / 16 : 4;      // 16 dims each: eight fragments of both key tiles in front of their products
 #pragma unroll
     for (int i0 = 0; i0 < DQ / 16; i0 += IG) {
@@ -311,43 +317,56 @@ struct Rows32 {
       for (int i = 0; i < IG; ++i)
 #pragma unroll
         for (int t = 0; t < KT / 32; ++t)
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t][i], qf[i0 + i], i0 + i == 0 ? floatx16{} : s[t], 0, 0, 0);
+#pragma unroll
+          for (int c = 0; c < NR; ++c)
+            s[c][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t][i], qf[c][i0 + i], i0 + i == 0 ? floatx16{} : s[c][t], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
     if (!whole) {
 #pragma unroll
+      for (int c = 0; c < NR; ++c)
+#pragma unroll
+        for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[c][t][r] = 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < left[c] ? s[c][t][r] : -INFINITY;
+    }
+    bool grown = false;
+    float m_new[NR];
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      float mx = s[c][0][0];
+#pragma unroll
       for (int t = 0; t < KT / 32; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][r] = 32 * t + 8 * (r / 4) + 4 * hh + r % 4 < left[0] ? s[t][r] : -INFINITY;
-    }
-    float mx = s[0][0];
-#pragma unroll
-    for (int t = 0; t < KT / 32; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r]);
-    {
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[c][t][r]);
       const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      mx = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+      m_new[c] = fmaxf(m[c], fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1])));
+      grown |= (m_new[c] - m[c]) * sc > RESCALE_LOG2;
     }
-    const float m_new = fmaxf(m[0], mx);
-    if (__builtin_amdgcn_ballot_w64((m_new - m[0]) * sc > RESCALE_LOG2) != 0ull) {
-      const float alpha = m[0] == m_new ? 1.f : __builtin_amdgcn_exp2f((m[0] - m_new) * sc);
-      m[0] = m_new;
-      l[0] *= alpha;
+    if (__builtin_amdgcn_ballot_w64(grown) != 0ull) {
 #pragma unroll
-      for (int u = 0; u < DV / 32; ++u)
+      for (int c = 0; c < NR; ++c) {
+        const float alpha = m[c] == m_new[c] ? 1.f : __builtin_amdgcn_exp2f((m[c] - m_new[c]) * sc);
+        m[c] = m_new[c];
+        l[c] *= alpha;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[u][r] *= alpha;
-    }
-    const float msc = (m[0] == -INFINITY ? 0.f : m[0]) * sc;
+        for (int u = 0; u < DV / 32; ++u)
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[t][r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][r + e], sc, -msc));
-        l[0] += (s[t][r] + s[t][r + 1]) + (s[t][r + 2] + s[t][r + 3]);
+          for (int r = 0; r < 16; ++r) o[c][u][r] *= alpha;
       }
+    }
+#pragma unroll
+    for (int c = 0; c < NR; ++c) {
+      const float msc = (m[c] == -INFINITY ? 0.f : m[c]) * sc;
+#pragma unroll
+      for (int t = 0; t < KT / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[c][t][r + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][t][r + e], sc, -msc));
+          l[c] += (s[c][t][r] + s[c][t][r + 1]) + (s[c][t][r + 2] + s[c][t][r + 3]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < KT / 32; ++i) {      // 32 keys: two products a block of dims
       TrnRegs vr[2][DV / 32];
@@ -355,19 +374,25 @@ struct Rows32 {
       for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int u = 0; u < DV / 32; ++u) trn_issue<DV>(vr[e][u], Vt, 32 * u, 2 * i + e);
-      bf16x8_t pf[2];
+      bf16x8_t pf[NR][2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        floatx8 p;
+      for (int c = 0; c < NR; ++c)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) p[r] = s[i][8 * e + r];
-        pf[e] = __builtin_convertvector(p, bf16x8_t);
-      }
+        for (int e = 0; e < 2; ++e) {
+          floatx8 p;
+#pragma unroll
+          for (int r = 0; r < 8; ++r) p[r] = s[c][i][8 * e + r];
+          pf[c][e] = __builtin_convertvector(p, bf16x8_t);
+        }
       trn_wait();
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int u = 0; u < DV / 32; ++u) o[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(trn_frag(vr[e][u]), pf[e], o[u], 0, 0, 0);
+        for (int u = 0; u < DV / 32; ++u) {
+          const bf16x8_t vf = trn_frag(vr[e][u]);
+#pragma unroll
+          for (int c = 0; c < NR; ++c) o[c][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[c][e], o[c][u], 0, 0, 0);
+        }
     }
   }
 };
@@ -447,14 +472,14 @@ __device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, 
     if (j + e < n) a.w_out[bh * a.cap + j + e] = before[e] + sum[e];
 }
 
-// Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64 or 128, 16 or 32 a wavefront, and every tile shared.
-enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3 };
+// Rows of an item: up to 16 or 32, its key tiles shared out over the wavefronts; up to 64, 128 or 256, 16, 32 or 64 a wavefront, and every tile shared.
+enum { ROWS_16 = 0, ROWS_32 = 1, ROWS_64 = 2, ROWS_128 = 3, ROWS_256 = 4 };
 // Key tiles, LDS buffers of NB stages and their bytes.  Shared tiles have 64 keys; a wavefront's own ones 32, so that two stages for four wavefronts take
 // as much as four stages of shared tiles.
 template <int DQ, int DV, int ROWS, int NB>
 struct PrefixShape {
   static constexpr bool SHARE = ROWS >= ROWS_64;
-  typedef std::conditional_t<ROWS == ROWS_128, Rows32<DQ, DV>, Rows16<DQ, DV, ROWS == ROWS_32 ? 2 : 1>> Rows;
+  typedef std::conditional_t<ROWS >= ROWS_128, Rows32<DQ, DV, ROWS == ROWS_256 ? 2 : 1>, Rows16<DQ, DV, ROWS == ROWS_32 ? 2 : 1>> Rows;
   static constexpr int KT = SHARE ? 64 : 32, ROW_TILE = 16 << ROWS;
   static constexpr int loop = (SHARE ? 1 : 4) * NB * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * Rows::COLS * (DV * 16 + 32) + Rows::COLS * 16) * 4;
   static constexpr int lds = loop > join ? loop : join;
@@ -643,7 +668,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 // The pairs that are built: items of one kind for every width; apart, own tiles beside the prefix's for narrow heads, and shared ones for wide heads,
 // where own tiles of every wavefront would leave a compute unit one workgroup (prefix_plan()).
 #define PREFIX_KINDS_ALL(X, DQ, DV) X(DQ, DV, ROWS_16, ROWS_16) X(DQ, DV, ROWS_32, ROWS_32) X(DQ, DV, ROWS_64, ROWS_64) X(DQ, DV, ROWS_128, ROWS_128)
-#define PREFIX_KINDS_NARROW(X, DQ, DV) X(DQ, DV, ROWS_16, ROWS_32) X(DQ, DV, ROWS_16, ROWS_64) X(DQ, DV, ROWS_32, ROWS_64) X(DQ, DV, ROWS_16, ROWS_128) X(DQ, DV, ROWS_32, ROWS_128)
+#define PREFIX_KINDS_NARROW(X, DQ, DV) X(DQ, DV, ROWS_16, ROWS_32) X(DQ, DV, ROWS_16, ROWS_64) X(DQ, DV, ROWS_32, ROWS_64) X(DQ, DV, ROWS_16, ROWS_128) X(DQ, DV, ROWS_32, ROWS_128) X(DQ, DV, ROWS_256, ROWS_256)
 #define PREFIX_KINDS_WIDE(X, DQ, DV) X(DQ, DV, ROWS_64, ROWS_128)
 constexpr bool prefix_wide(int dq, int dv) { return dq + dv > 128; }
 template <int DQ, int DV, int OWN, int PREFIX>

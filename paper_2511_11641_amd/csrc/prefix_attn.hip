@@ -187,19 +187,20 @@ struct PrefixPlan {
 };
 
 // What the items of a call cost, in ns, for the choice between ways to cut it.  Constants as measured: an item's start and end 3 us, a step's least
-// time (a latency of memory), 5.5 bytes/ps of memory over all workgroups, and a row and key of a tile on a compute unit (heads of 64 + 64 dims 0.08 ns:
-// prompts of 16 x 509 tokens; the unused rows of a tile cost as much).
+// time (a latency of memory, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5 bytes/ps of memory over all workgroups (`share` of them read the same keys), and a row and key of a tile on a
+// compute unit (heads of 64 + 64 dims 0.08 ns; the unused rows of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them
+// such items.
 struct ItemCost { double step, item; };
-static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double active) {
-  const double keys = keys_of(kind) * tiles_at_once(kind), per_cu = std::ceil(active / 256);
-  const double memory = active * keys * (a.kq + a.kv) * 2 / 5500, compute = per_cu * rows_of(kind) * keys * (0.02 + 0.0005 * (p.dq + p.dv));
-  double step = 900;
+static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double keys, double active, double alike, double share) {
+  const double per_cu = std::ceil(alike / 256), step_keys = keys_of(kind) * tiles_at_once(kind), pair = (0.02 + 0.0005 * (p.dq + p.dv)) * (kind == ROWS_256 ? 0.92 : 1);
+  const double memory = active * (keys < step_keys ? keys : step_keys) * (a.kq + a.kv) * 2 / (5500 * share), compute = per_cu * rows_of(kind) * step_keys * pair;
+  double step = kind >= ROWS_64 ? (kind == ROWS_64 ? 0.7 : (kind == ROWS_128 ? 1 : 1.7)) * (600 + 6 * (p.dq + p.dv)) : 900;      // a wavefront by itself
   if (memory > step) step = memory;
   if (compute > step) step = compute;
   return {step, 3000 + steps * step};
 }
 static double join_cost(const PrefixArgs& a, int slots) {
-  return slots > 1 ? 4000 + static_cast<double>(a.h_kv) * a.rows * slots * (a.kv + 2) * 8 / 4000 : 0;
+  return slots > 1 ? 3000 + static_cast<double>(a.h_kv) * a.rows * slots * (a.kv + 2) * 8 / 5000 : 0;
 }
 static inline long long ceil_div(long long x, long long y) { return (x + y - 1) / y; }
 
@@ -211,8 +212,9 @@ static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
   long long best_chunk = 0;
   for (long long chunks = 1; chunks <= 64 && (chunks == 1 || ceil_div(steps, chunks) >= 2); chunks += (chunks < 8 ? 1 : chunks / 4)) {
     const long long chunk = steps > 0 ? ceil_div(steps, chunks) : 1, n = steps > 0 ? ceil_div(steps, chunk) : 1, wgs = pairs * n;
-    const ItemCost c = item_cost(a, p, p.own, static_cast<double>(chunk), static_cast<double>(wgs < resident ? wgs : resident));
-    const double cost = static_cast<double>(ceil_div(wgs, resident)) * c.item + join_cost(a, static_cast<int>(n));
+    const double active = static_cast<double>(wgs < resident ? wgs : resident), rounds = wgs <= resident ? 1 : static_cast<double>(wgs) / resident + 0.15;
+    const ItemCost c = item_cost(a, p, p.own, static_cast<double>(chunk), static_cast<double>(a.P + a.own_max) / n, active, active, a.o_row_tiles);
+    const double cost = rounds * c.item + join_cost(a, static_cast<int>(n));
     if (best_chunk == 0 || cost < best) { best = cost; best_chunk = chunk; }
   }
   if (set) {
@@ -239,7 +241,8 @@ static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
       const long long p_n = ceil_div(p_steps, p_chunk), o_n = ceil_div(o_steps, o_chunk);
       const double p_wgs = static_cast<double>(a.h_kv * row_tiles * p_n), o_wgs = static_cast<double>(pairs * o_n), wgs = p_wgs + o_wgs;
       const double active = wgs < resident ? wgs : static_cast<double>(resident);
-      const ItemCost cp = item_cost(a, p, prefix, static_cast<double>(p_chunk), active), co = item_cost(a, p, p.own, static_cast<double>(o_chunk), active);
+      const ItemCost cp = item_cost(a, p, prefix, static_cast<double>(p_chunk), static_cast<double>(a.P) / p_n, active, active * p_wgs / wgs, static_cast<double>(row_tiles));
+      const ItemCost co = item_cost(a, p, p.own, static_cast<double>(o_chunk), static_cast<double>(a.own_max) / (o_n > 0 ? o_n : 1), active, active * o_wgs / wgs, 1);
       const double longest = cp.item > co.item ? cp.item : co.item, all = (p_wgs * cp.item + o_wgs * co.item) / resident;
       const double cost = (all > longest ? all + longest / 4 : longest) + join_cost(a, static_cast<int>(p_n + o_n));
       if (best_p == 0 || cost < best) { best = cost; best_p = p_chunk; best_o = o_chunk; }
@@ -284,6 +287,13 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   } else {
     p.own = own;
     plan_joint(a, p, resident_joint, true);
+    // Prompts: 64 rows a wavefront halve the reads of LDS, where narrow heads leave the registers and there are workgroups enough for two on every
+    // compute unit several times over (16 x 509 tokens on 8192, 4 query heads a key/value head: 674 -> 627 us; 8 x 256 on 2048: 43 -> 48).
+    if (own == ROWS_128 && !prefix_wide(p.dq, p.dv) && a.slots == 0 && static_cast<long long>(a.B) * a.h_kv * ceil_div(a.own_rows, 256) >= 1024) {
+      p.own = ROWS_256;
+      a.o_row_tiles = static_cast<int>(ceil_div(a.own_rows, 256));
+      plan_joint(a, p, 512, true);
+    }
   }
   // the kernels cut the keys as the plan did
   if (a.p_tiles != ceil_div(a.P, keys_of(p.prefix)) || p.prefix < p.own) return false;

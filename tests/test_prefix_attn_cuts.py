@@ -9,8 +9,8 @@ import pytest
 from paper_2511_11641_amd import binding as B
 
 FIELDS = ("joint", "p_tiles", "p_chunks", "p_chunk", "p_row_tiles", "p_items", "o_chunks", "o_chunk", "o_row_tiles", "slots", "own", "prefix", "grid", "weigh", "own_pad", "keep")
-ROWS, KEYS, AT_ONCE = (16, 32, 64, 128), (32, 32, 64, 64), (4, 4, 1, 1)
-SAME, NARROW, WIDE = {(0, 0), (1, 1), (2, 2), (3, 3)}, {(0, 1), (0, 2), (1, 2), (0, 3), (1, 3)}, {(2, 3)}      # the kernels that are built
+ROWS, KEYS = (16, 32, 64, 128, 256), (32, 32, 64, 64, 64)
+SAME, NARROW, WIDE = {(0, 0), (1, 1), (2, 2), (3, 3)}, {(0, 1), (0, 2), (1, 2), (0, 3), (1, 3), (4, 4)}, {(2, 3)}      # the kernels that are built
 
 
 def cut(lib, Bn, L, h, h_kv, e, f, P, own_max, weights=1):
@@ -55,7 +55,7 @@ def check(lib, Bn, L, h, h_kv, e, f, P, own_max, lens, weights):
     own_rows, rows = L * g, Bn * L * g
     width = lambda n: 32 if n <= 32 else (64 if n <= 64 else 128)
     assert (a["own"], a["prefix"]) in SAME | (WIDE if width(e) + width(f) > 128 else NARROW) and a["p_tiles"] == -(-P // KEYS[a["prefix"]])
-    assert ROWS[a["own"]] >= min(own_rows, 128) and a["o_row_tiles"] == -(-own_rows // ROWS[a["own"]])
+    assert a["own"] == 4 or ROWS[a["own"]] >= min(own_rows, 128) and a["o_row_tiles"] == -(-own_rows // ROWS[a["own"]])
     assert a["own_pad"] >= -(-own_max // KEYS[a["own"]]) * KEYS[a["own"]] and a["own_pad"] % 4 == 0
     if a["keep"]:
         assert a["o_row_tiles"] == 1 and own_rows <= 32 and (a["weigh"] > 0) == (a["slots"] > 0)
@@ -112,7 +112,8 @@ def test_every_row_meets_every_key_once(lib, seed):
 
 
 @pytest.mark.parametrize("shape", [(64, 1, 8, 2, 64, 64, 9000, 512), (12, 5, 4, 4, 96, 128, 8191, 300), (32, 1, 4, 4, 32, 32, 4096, 500), (4, 1, 8, 2, 64, 64, 20000, 64),
-                                   (1, 1, 8, 2, 64, 64, 30000, 100), (40, 1, 4, 1, 128, 128, 3000, 700), (9, 2, 16, 2, 128, 96, 2500, 90), (24, 2, 4, 2, 32, 48, 1, 2000)])
+                                   (1, 1, 8, 2, 64, 64, 30000, 100), (40, 1, 4, 1, 128, 128, 3000, 700), (9, 2, 16, 2, 128, 96, 2500, 90), (24, 2, 4, 2, 32, 48, 1, 2000),
+                                   (16, 70, 128, 32, 64, 64, 200, 90), (3, 600, 2, 1, 32, 64, 700, 601)])
 def test_long_prefixes_and_batches(lib, shape):
     Bn, own_max = shape[0], shape[-1]
     check(lib, *shape, [own_max - 31 * i % (own_max + 1) for i in range(Bn)], 1)
