@@ -215,8 +215,10 @@ extern "C" int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src, cons
   if ((n + 511) / 512 > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
   a.small = n < 1 << 27;
   a.per_inv = static_cast<unsigned>(((1ll << 32) + per - 1) / per);
-  // Small caches: the launch saved outweighs the copying that one workgroup a cache does more slowly.
-  if (n * 16 <= 128 * 1024) {
+  // Small caches: the launch saved outweighs the copying that one workgroup a cache does more slowly (one launch against two, 64 + 64 dims, 4 / 64 /
+  // 256 caches: 32 KB each 8.2 / 9.4 / 11.6 us against 8.7 / 9.5 / 12.8, 64 KB 9.4 / 10.5 / 14.3 against 8.8 / 10.7 / 15.3, 128 KB 11.3 / 16.4 / 20.7
+  // against 9.0 / 12.3 / 21.9; issued one by one from the host a launch more costs 1.4 us where there is little else).
+  if (n * 16 <= 64 * 1024) {
     hipLaunchKernelGGL(cache_evict_kernel, dim3(groups), dim3(SELECT_THREADS), 0, ctx->stream, a);
     ECOSPA_CHECK_LAUNCH(ctx, "cache_evict_kernel");
     return ECOSPA_OK;

@@ -1,10 +1,13 @@
 // Penalties, biases, temperature and masks on logits, with the best token and the log-sum-exp of every row.
 //
-// A workgroup takes a range of the vocabulary of one row.  It asks for all of its logits first - 8 or 16 a thread stay in registers - and for
+// A workgroup takes a range of the vocabulary of one row.  It asks for all of its logits first - 8, 16 or 32 a thread stay in registers - and for
 // the head of the history, and counts, while the logits travel, the row's history and bias entries that fall into its range in LDS (integer
 // atomics: the order does not show).  Then every thread transforms and stores its logits; maximum, its lowest token and the sum of
-// exponentials come from the registers, without a second look at memory.  The ranges' results of a row are joined by a second launch (none where one range is the row).  Nothing is added in an
-// order that varies: results repeat bit for bit.
+// exponentials come from the registers, without a second look at memory.  The ranges' results of a row are joined by a second launch (none where
+// one range is the row).  Nothing is added in an order that varies: results repeat bit for bit.
+//
+// The penalties, a temperature and the exponential are about 50 vector instructions a logit, beside 4 to 8 bytes of memory: 256 x 131072 fp32 with
+// histories of 8192 take 77 us, 3.5 TB/s, and with histories of 100 63 us, 4.3 TB/s.  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
 #include "common.h"
 
 #define LOGITS_COUNTS 22               // a counter's low bits: occurrences in the history; above them: the last bias entry of the token, from 1
@@ -252,13 +255,15 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsArgs a) {
 
 // Threads, logits a thread and tokens of a workgroup.  A vocabulary that one workgroup holds needs no join (256 x 9000 bf16, histories of 2000:
 // one range of 1024 threads 7.4 us, two of 512 and the join 9.9).  Else 16 logits a thread in workgroups of 512, of which a compute unit holds four
-// (256 x 131072 fp32, histories of 8192: 76 us; 32 a thread 80, 8 a thread 95), and 8 in workgroups of 256 while all of them are resident at once
-// and shorter passes end sooner (1 x 32000: 5.8 us against 7.0; 64 x 32000 8.6 against 8.7).
+// (256 x 131072 fp32, histories of 8192: 77 us; 32 a thread 80, 8 a thread 95; workgroups of 1024 76, but 256 x 50257 bf16 23.5 against 21.8), and 8
+// in workgroups of 256 while all of them are resident at once and shorter passes end sooner (1 x 32000: 5.8 us against 7.0; 64 x 32000 8.6 against
+// 8.7).  With rows for most compute units one workgroup also holds twice as many, 32 a thread: the join is saved and the history read once (bf16 x
+// 32000, histories of 1000: 256 rows 13.6 us against 16.0, 160 rows 12.3 against 13.2, but 128 rows 11.9 against 11.2 and one row 9.1 against 5.9).
 struct LogitsPlan { int threads, each, range, ranges; };
 static LogitsPlan logits_plan(int B, int V) {
   LogitsPlan p;
-  const bool one = V <= 1024 * 16, few = !one && static_cast<long long>(B) * V <= 1 << 21;
-  p.each = few ? 8 : 16;
+  const bool twice = V > 1024 * 16 && V <= 1024 * 32 && B >= 160, one = V <= 1024 * 16 || twice, few = !one && static_cast<long long>(B) * V <= 1 << 21;
+  p.each = few ? 8 : (twice ? 32 : 16);
   p.threads = few ? 256 : (!one ? 512 : (V <= 256 * 16 ? 256 : (V <= 512 * 16 ? 512 : 1024)));
   p.ranges = (V + p.threads * p.each - 1) / (p.threads * p.each);
   p.range = ((V + p.ranges - 1) / p.ranges + 31) / 32 * 32;
@@ -280,12 +285,14 @@ static hipError_t logits_launch_as(const LogitsArgs& a, hipStream_t st) {
 }
 template <typename T, typename U>
 static hipError_t logits_launch(const LogitsArgs& a, const LogitsPlan& p, hipStream_t st) {
+  if (p.each == 32) return logits_launch_as<T, U, 1024, 32>(a, st);
   if (p.each == 8) return logits_launch_as<T, U, 256, 8>(a, st);
   return p.threads == 256 ? logits_launch_as<T, U, 256, 16>(a, st) : (p.threads == 512 ? logits_launch_as<T, U, 512, 16>(a, st) : logits_launch_as<T, U, 1024, 16>(a, st));
 }
 #define LOGITS_INSTANTIATE(T, U)                                                                                                          \
   template __global__ void logits_kernel<T, U, 256, 8>(const LogitsArgs); template __global__ void logits_kernel<T, U, 256, 16>(const LogitsArgs); \
-  template __global__ void logits_kernel<T, U, 512, 16>(const LogitsArgs); template __global__ void logits_kernel<T, U, 1024, 16>(const LogitsArgs);
+  template __global__ void logits_kernel<T, U, 512, 16>(const LogitsArgs); template __global__ void logits_kernel<T, U, 1024, 16>(const LogitsArgs); \
+  template __global__ void logits_kernel<T, U, 1024, 32>(const LogitsArgs);
 LOGITS_INSTANTIATE(bf16_t, bf16_t) LOGITS_INSTANTIATE(bf16_t, float) LOGITS_INSTANTIATE(float, bf16_t) LOGITS_INSTANTIATE(float, float)
 #undef LOGITS_INSTANTIATE
 

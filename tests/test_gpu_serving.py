@@ -295,6 +295,39 @@ def test_logits(ctx, V, dt, odt):
     assert torch.equal(buf[:, :V].cpu(), torch.from_numpy(want).float().to(types[dt]))
 
 
+@pytest.mark.parametrize("V", [16385, 20001, 32768])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_logits_of_many_rows(ctx, V, dt):
+    """Rows for most of the chip, a vocabulary that one workgroup holds then: every row as the definition, exactly."""
+    distinct, Bn, H = 5, 163, 900
+    rng = np.random.default_rng(V)
+    t = {"bf16": torch.bfloat16, "f32": torch.float32}[dt]
+    of = np.arange(Bn) % distinct
+    x = rng.integers(-64, 65, (distinct, V)) / 8.0
+    x[1, [V - 1, V - 7]] = 20.0                                         # the lower of equal ones, in the last chunk
+    hist = rng.integers(0, V, (distinct, H))
+    hist[1] %= V - 7
+    hist[:, ::3] = hist[:, :1]
+    ids = np.stack([rng.choice(V, 9, replace=False) for _ in range(distinct)])
+    ids[1] %= V - 7
+    ids[:, 7] = ids[:, 2]
+    mask = rng.integers(0, 1 << 32, (2, (V + 31) // 32), dtype=np.uint64).astype(np.uint32).view(np.int32)
+    mask[1] = 0
+    ref = dict(history=hist, repetition=np.array([1, 2, 4, 2, 0.5]), frequency=np.array([0, 0.25, 0.5, 1, 0.25]), presence=np.array([0.5, 0, 0.25, 0, 1]),
+               temperature=np.array([1, 2, 0.5, 4, 1]), bias_ids=ids, bias=rng.integers(-8, 9, (distinct, 9)) / 4.0, mask=mask, mask_row=np.array([0, -1, 0, 1, 2]))
+    want, pick, lse = S.logits_process(x, **ref)
+    up = lambda n, a: torch.from_numpy(np.ascontiguousarray(a if n == "mask" else a[of])).to(torch.int32 if a.dtype.kind == "i" and n != "temperature" else torch.float32).cuda()
+    buf = torch.full((Bn, (V + 7) // 8 * 8 + 8), float("nan"), device="cuda", dtype=t)
+    buf[:, :V] = torch.from_numpy(x[of]).to(t).cuda()
+    out = torch.full_like(buf, 77.0)
+    got_pick, got_lse = ctx.ecospa_logits_process(buf[:, :V], out=out[:, :V], **{n: up(n, a) for n, a in ref.items()})
+    assert torch.equal(out[:, :V].cpu(), torch.from_numpy(want[of]).float().to(t)) and (out[:, V:] == 77).all()
+    assert got_pick.tolist() == pick[of].tolist() and pick[1] == V - 7
+    got, lse = got_lse.double().cpu().numpy(), lse[of]
+    fine = np.isfinite(lse)
+    assert np.array_equal(got[~fine], lse[~fine]) and (np.abs(got[fine] - lse[fine]) <= 2.0 ** -19 * (2 + np.abs(lse[fine]))).all()
+
+
 def test_logits_values_and_ties(ctx):
     V = 9000
     x = torch.zeros(6, V, device="cuda")
