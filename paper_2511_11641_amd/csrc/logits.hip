@@ -237,14 +237,15 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsArgs a) {
   const int b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (b >= a.q.B) return;
   const LogitsPart* const p = a.part + static_cast<long long>(b) * a.ranges;
-  float m = -INFINITY;
-  for (int i = lane; i < a.ranges; i += 64) m = fmaxf(m, p[i].m);
+  LogitsPart x = p[min(lane, a.ranges - 1)];      // up to 64 ranges are read once
+  float m = x.m;
+  for (int i = lane + 64; i < a.ranges; i += 64) m = fmaxf(m, p[i].m);
   m = wave_max(m);
   const float ref = m == -INFINITY ? 0.f : m;
   float s = 0.f;
   uint32_t at = 0xffffffffu;
   for (int i = lane; i < a.ranges; i += 64) {
-    const LogitsPart x = p[i];
+    if (i > lane) x = p[i];
     s += x.s * (x.m == m && m != -INFINITY ? 1.f : __expf(x.m - ref));
     if (x.m == m && x.at >= 0) at = min(at, static_cast<uint32_t>(x.at));
   }
