@@ -40,6 +40,7 @@ struct PrefixArgs {
   int p_chunks, p_chunk, p_row_tiles;      // prefix items: chunks, key tiles of a chunk, tiles of rows
   int o_chunks, o_chunk, o_row_tiles;      // own (or joint) items
   int p_items;             // prefix items in front of the others in the grid
+  int own_once, prefix_once;      // keys that one item reads, too many to stay in the last cache: their loads pass the caches by
   int slots;               // pieces per row in the workspace; 0: every item is all of its rows
   float* scores;           // workspace: [B][h_kv][own_rows][own_pad] scores of the own keys times scale * log2 e, null: not wanted
   int own_pad;
@@ -68,6 +69,7 @@ struct KvLoader {
 #pragma unroll
     for (int i = 0; i < NC; ++i) col[i] = static_cast<unsigned>(min(((lane % CPR) ^ nat_swz<D>(row0 + i * RPI)) * 8, kp - 8) * 2);
   }
+  template <int AUX>      // 0, or 2: past the caches
   __device__ __forceinline__ void issue(bf16_t* tile, const char* base, unsigned ldb, int valid) const {
     lds_bf16_t* const dst = (lds_bf16_t*)tile + wave * (PER * 512);
     if (valid >= KT) {
@@ -76,14 +78,14 @@ struct KvLoader {
       for (int i = 0; i < PER; ++i) {
         unsigned o = at + col[i % NC];
         asm volatile("" : "+v"(o));      // keeps the offset a lane register at the load
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + static_cast<unsigned long long>(i * RPI) * ldb + o), dst + i * 512, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + static_cast<unsigned long long>(i * RPI) * ldb + o), dst + i * 512, 16, 0, AUX);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         unsigned o = static_cast<unsigned>(min(row0 + i * RPI, valid - 1)) * ldb + col[i % NC];
         asm volatile("" : "+v"(o));
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + o), dst + i * 512, 16, 0, 0);
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<const void*>(base + o), dst + i * 512, 16, 0, AUX);
       }
     }
   }
@@ -512,8 +514,14 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
     const int valid = (own ? it.own_n : a.P) - static_cast<int>(first);
     const long long ldk = 2 * (own ? a.k_st : a.pk_st), ldv = 2 * (own ? a.v_st : a.pv_st);
     bf16_t* const at = buf + n * (KT * (DQ + DV));
-    kl.issue(at, (own ? ok : pk) + first * ldk, static_cast<unsigned>(ldk), valid);
-    vl.issue(at + KT * DQ, (own ? ov : pv) + first * ldv, static_cast<unsigned>(ldv), valid);
+    const char *const kb = (own ? ok : pk) + first * ldk, *const vb = (own ? ov : pv) + first * ldv;
+    if (own ? a.own_once : a.prefix_once) {
+      kl.template issue<2>(at, kb, static_cast<unsigned>(ldk), valid);
+      vl.template issue<2>(at + KT * DQ, vb, static_cast<unsigned>(ldv), valid);
+    } else {
+      kl.template issue<0>(at, kb, static_cast<unsigned>(ldk), valid);
+      vl.template issue<0>(at + KT * DQ, vb, static_cast<unsigned>(ldv), valid);
+    }
   };
   constexpr int STEP = SHARE ? 1 : 4;
   const int first = it.t0 + (SHARE ? 0 : wave);

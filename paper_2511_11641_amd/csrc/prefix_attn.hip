@@ -295,6 +295,10 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
       plan_joint(a, p, 512, true);
     }
   }
+  // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call: their loads pass the caches by.
+  const auto once = [&](double heads, double keys, int row_tiles) { return row_tiles == 1 && heads * keys * (a.kq + a.kv) * 2 > 96e6; };
+  a.own_once = once(static_cast<double>(a.B) * a.h_kv, a.own_max, a.o_row_tiles);
+  a.prefix_once = once(a.h_kv, a.P, a.joint ? a.B * a.o_row_tiles : a.p_row_tiles);
   // the kernels cut the keys as the plan did
   if (a.p_tiles != ceil_div(a.P, keys_of(p.prefix)) || p.prefix < p.own) return false;
   // The weights need every own score against a sum that is complete only at the end.  Kept scores are written and read, 8 bytes a row and key;

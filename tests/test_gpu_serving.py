@@ -177,6 +177,16 @@ def test_attention_past_32_bits(ctx):
     assert torch.equal(ko[0, 0], c.k[0, 0, 6:]) and torch.equal(vo[0, 0], c.v[0, 0, 6:]) and lens.item() == 64
 
 
+@pytest.mark.parametrize("Bn,L,h,h_kv,e,f,P,lens,cap", [
+    (3, 1, 8, 4, 48, 48, 100, [200, 33, 0], 50000), (2, 40, 4, 2, 48, 64, 77, [90, 40], 110000), (2, 1, 4, 2, 128, 96, 0, [70, 1], 60000),
+    (1, 1, 4, 2, 48, 48, 262000, [10], 20), (5, 1, 4, 2, 64, 32, 262001, [10, 0, 3, 70, 1], 80), (4, 3, 4, 2, 96, 128, 110001, [3, 50, 9, 0], 60)])
+def test_attention_of_large_caches(ctx, Bn, L, h, h_kv, e, f, P, lens, cap):
+    """More than 96 MB of keys and values in own caches or in the prefix, each read by one item: loads that pass the caches by."""
+    assert 2 * h_kv * (e + f) * max(Bn * cap, P) > 96e6
+    c = Case(11, Bn, L, h, h_kv, e, f, P, lens, cap=cap)
+    c.check(*c.run(ctx))
+
+
 # ---- append -------------------------------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("rope", [False, True])
 @pytest.mark.parametrize("Bn,L,h,h_kv,e,f,cap,lens", [(1, 1, 1, 1, 16, 16, 1, [1]), (4, 1, 16, 16, 32, 32, 40, [1, 40, 7, 0]), (3, 5, 8, 2, 48, 128, 20, [5, 20, 3]),
