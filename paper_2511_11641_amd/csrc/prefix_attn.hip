@@ -4,9 +4,10 @@
 #include <cmath>
 
 // ---------------------------------------------------------------------------------------------
-// Join.  Threads are (piece, four dims): a thread weighs its pieces against the maximum of its own, four of them asked for at a time, before it is
-// known how many there are (what counts is how many latencies follow on each other).  FEW pieces: W threads take a row by themselves.  Otherwise a
-// workgroup does, and its threads of equal dims are added up against the row's maximum in a fixed order.
+// Join.  Bound by latency: launch, statistics, pieces, result (64 requests x 32 heads of 16 pieces of 64 dims, with the weights of 2048 own keys each, 42
+// MB in all: 10 us; 32 x 32 heads of 7 pieces of 32 dims 3.5 us).  Threads are (piece, four dims): a thread weighs its pieces against the maximum of its
+// own, four of them asked for at a time, before it is known how many there are (what counts is how many latencies follow on each other).  FEW pieces: W
+// threads take a row by themselves.  Otherwise a workgroup does, and its threads of equal dims are added up against the row's maximum in a fixed order.
 // ---------------------------------------------------------------------------------------------
 // Pieces that the items left of the rows of request b from `in` on (a row of the request's): as prefix_item() cuts them.
 __device__ __forceinline__ int prefix_pieces(const PrefixArgs& a, int b, int in, int kt, int row_tile) {
@@ -120,7 +121,8 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
 
 // ---------------------------------------------------------------------------------------------
 // Weights: w_out[j] = w_in[j] + sum over the rows of the request that see own key j of exp(s_j - lse).  A wavefront takes 32 keys: their fragments
-// stay in registers while the rows pass by, 16 at a time; the sum over a tile's rows is a sum over lanes.
+// stay in registers while the rows pass by, 16 at a time; the sum over a tile's rows is a sum over lanes.  Bound like the scores' part of the
+// attention, at half its products; taken where keeping scores would move more (many rows a request: prompts).
 // ---------------------------------------------------------------------------------------------
 template <int DQ>
 __global__ __launch_bounds__(256) void prefix_weights_kernel(const PrefixArgs a, const float* lse, const float* w_in, float* w_out, int cap) {
@@ -187,12 +189,15 @@ struct PrefixPlan {
 };
 
 // What the items of a call cost, in ns, for the choice between ways to cut it.  Constants as measured: an item's start and end 3 us, a step's least
-// time (a latency of memory, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5 bytes/ps of memory over all workgroups (`share` of them read the same keys), and a row and key of a tile on a
-// compute unit (heads of 64 + 64 dims 0.08 ns; the unused rows of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them
-// such items.
+// time (a latency of memory, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5 bytes/ps of memory over
+// all workgroups (`share` of them read the same keys), and a row and key of a tile on a compute unit (heads of 64 + 64 dims 0.08 ns; the unused rows
+// of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them such items.  Chunks of the prefix forced to other counts
+// (8 to 48, 1 and 2 of own keys): the choice is within 1 % of the best for 64 requests on 32768 tokens (15 chosen, 12 best; with weights 81 us
+// against 77), for 12 x 5 on 8191 and 8 on 2000 the best, for 32 on 4096 21.0 us against 19.4 (6 chosen, 3 best).
 struct ItemCost { double step, item; };
 static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double keys, double active, double alike, double share) {
-  const double per_cu = std::ceil(alike / 256), step_keys = keys_of(kind) * tiles_at_once(kind), pair = (0.02 + 0.0005 * (p.dq + p.dv)) * (kind == ROWS_256 ? 0.92 : 1);
+  const double per_cu = std::ceil(alike / 256), step_keys = keys_of(kind) * tiles_at_once(kind);
+  const double pair = (0.02 + 0.0005 * (p.dq + p.dv)) * (kind == ROWS_256 ? 0.92 : 1);
   const double memory = active * (keys < step_keys ? keys : step_keys) * (a.kq + a.kv) * 2 / (5500 * share), compute = per_cu * rows_of(kind) * step_keys * pair;
   double step = kind >= ROWS_64 ? (kind == ROWS_64 ? 0.7 : (kind == ROWS_128 ? 1 : 1.7)) * (600 + 6 * (p.dq + p.dv)) : 900;      // a wavefront by itself
   if (memory > step) step = memory;
@@ -207,7 +212,8 @@ static inline long long ceil_div(long long x, long long y) { return (x + y - 1) 
 // Items that run over the prefix and then the own keys of their request: `chunks` of them per tile of rows.
 static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool set) {
   const int kt = keys_of(p.own), at_once = tiles_at_once(p.own);
-  const long long pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles, tiles = ceil_div(a.P, kt) + ceil_div(a.own_max, kt), steps = ceil_div(tiles, at_once);
+  const long long pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles;
+  const long long tiles = ceil_div(a.P, kt) + ceil_div(a.own_max, kt), steps = ceil_div(tiles, at_once);
   double best = 0;
   long long best_chunk = 0;
   for (long long chunks = 1; chunks <= 64 && (chunks == 1 || ceil_div(steps, chunks) >= 2); chunks += (chunks < 8 ? 1 : chunks / 4)) {
@@ -230,7 +236,8 @@ static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
 }
 // Items of the prefix for the rows of all requests, and items of own keys.
 static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool set) {
-  const int prefix = kind_of(a.rows) < p.own ? p.own : kind_of(a.rows), kt = keys_of(p.own), at_once = tiles_at_once(p.own), kt_p = keys_of(prefix), at_once_p = tiles_at_once(prefix);
+  const int prefix = kind_of(a.rows) < p.own ? p.own : kind_of(a.rows), kt_p = keys_of(prefix), at_once_p = tiles_at_once(prefix);
+  const int kt = keys_of(p.own), at_once = tiles_at_once(p.own);
   const long long row_tiles = ceil_div(a.rows, rows_of(prefix)), pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles;
   const long long p_steps = ceil_div(ceil_div(a.P, kt_p), at_once_p), o_steps = ceil_div(ceil_div(a.own_max, kt), at_once);
   double best = 0;
@@ -241,8 +248,9 @@ static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
       const long long p_n = ceil_div(p_steps, p_chunk), o_n = ceil_div(o_steps, o_chunk);
       const double p_wgs = static_cast<double>(a.h_kv * row_tiles * p_n), o_wgs = static_cast<double>(pairs * o_n), wgs = p_wgs + o_wgs;
       const double active = wgs < resident ? wgs : static_cast<double>(resident);
-      const ItemCost cp = item_cost(a, p, prefix, static_cast<double>(p_chunk), static_cast<double>(a.P) / p_n, active, active * p_wgs / wgs, static_cast<double>(row_tiles));
-      const ItemCost co = item_cost(a, p, p.own, static_cast<double>(o_chunk), static_cast<double>(a.own_max) / (o_n > 0 ? o_n : 1), active, active * o_wgs / wgs, 1);
+      const double p_keys = static_cast<double>(a.P) / p_n, o_keys = static_cast<double>(a.own_max) / (o_n > 0 ? o_n : 1);
+      const ItemCost cp = item_cost(a, p, prefix, static_cast<double>(p_chunk), p_keys, active, active * p_wgs / wgs, static_cast<double>(row_tiles));
+      const ItemCost co = item_cost(a, p, p.own, static_cast<double>(o_chunk), o_keys, active, active * o_wgs / wgs, 1);
       const double longest = cp.item > co.item ? cp.item : co.item, all = (p_wgs * cp.item + o_wgs * co.item) / resident;
       const double cost = (all > longest ? all + longest / 4 : longest) + join_cost(a, static_cast<int>(p_n + o_n));
       if (best_p == 0 || cost < best) { best = cost; best_p = p_chunk; best_o = o_chunk; }
@@ -288,14 +296,17 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
     p.own = own;
     plan_joint(a, p, resident_joint, true);
     // Prompts: 64 rows a wavefront halve the reads of LDS, where narrow heads leave the registers and there are workgroups enough for two on every
-    // compute unit several times over (16 x 509 tokens on 8192, 4 query heads a key/value head: 674 -> 627 us; 8 x 256 on 2048: 43 -> 48).
+    // compute unit several times over (16 x 509 tokens on 8192, 4 query heads a key/value head: 653 -> 618 us; 8 x 256 on 2048 with its half as
+    // many workgroups: 43 -> 48).
     if (own == ROWS_128 && !prefix_wide(p.dq, p.dv) && a.slots == 0 && static_cast<long long>(a.B) * a.h_kv * ceil_div(a.own_rows, 256) >= 1024) {
       p.own = ROWS_256;
       a.o_row_tiles = static_cast<int>(ceil_div(a.own_rows, 256));
       plan_joint(a, p, 512, true);
     }
   }
-  // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call: their loads pass the caches by.
+  // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call: their loads pass the caches by.  Own
+  // caches of 134 MB 27.5 -> 23.9 us, 100 MB 21.6 -> 19.9, 268 MB 51.4 -> 44.5; a prefix of 268 MB 55.0 -> 48.0.  With 67 MB it depends on what
+  // passes between two calls: 17.2 -> 15.2 where the cache had lost them, 14.0 -> 14.9 where it had not.
   const auto once = [&](double heads, double keys, int row_tiles) { return row_tiles == 1 && heads * keys * (a.kq + a.kv) * 2 > 96e6; };
   a.own_once = once(static_cast<double>(a.B) * a.h_kv, a.own_max, a.o_row_tiles);
   a.prefix_once = once(a.h_kv, a.P, a.joint ? a.B * a.o_row_tiles : a.p_row_tiles);
@@ -342,7 +353,7 @@ int ecospa_cache_check(const ecospa_cache* c) {
   if (c->dtype != ECOSPA_BF16) return ECOSPA_ERR_DTYPE;
   if (c->B < 1 || c->h_kv < 1 || c->h < c->h_kv || c->h % c->h_kv || c->cap < 1 || c->own_max < 0 || c->own_max > c->cap || c->P < 0) return ECOSPA_ERR_SHAPE;
   if (c->kp_qk < 16 || c->kp_qk > 128 || c->kp_qk % 16 || c->kp_vo < 16 || c->kp_vo > 128 || c->kp_vo % 16) return ECOSPA_ERR_SHAPE;
-  if (!(c->scale > 0.f) || c->scale > 3.0e38f) return ECOSPA_ERR_SHAPE;
+  if (!(c->scale > 0.f) || c->scale > 2.0e38f) return ECOSPA_ERR_SHAPE;
   const long long rows[4] = {c->k_st, c->v_st, c->P > 0 ? c->pk_st : 1ll << 20, c->P > 0 ? c->pv_st : 1ll << 20};
   for (int i = 0; i < 4; ++i)      // 64 rows of a tile stay within 32 bits of bytes
     if (rows[i] < (i & 1 ? c->kp_vo : c->kp_qk) || rows[i] >= 1ll << 25) return ECOSPA_ERR_SHAPE;

@@ -96,6 +96,13 @@ def test_evict_refusals(lib, ctx):
     assert call(idx=None) == B.ERR_WORKSPACE
 
 
+def test_evict_refuses_its_inputs_as_outputs(lib, ctx):
+    src, dst = cache(lens=4096), cache(cap=20, own_max=0)
+    call = lambda lens, w_out: lib.ecospa_cache_evict(ctx, C.byref(src), 256, 10, 2, C.byref(dst), lens, w_out, None)
+    assert call(4096, None) == call(512, 256) == B.ERR_SHAPE
+    assert call(512, 768) == B.ERR_WORKSPACE
+
+
 def test_logits_refusals(lib, ctx):
     def call(x=ctx, **kw):
         q = B.Logits(2, 100, B.BF16, B.BF16, 256, 512, 104, 104, None, None, 0, 0, None, None, None, None, None, None, None, None, 0, 0, 1024, 2048)
