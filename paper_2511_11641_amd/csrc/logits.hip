@@ -7,7 +7,8 @@
 // one range is the row).  Nothing is added in an order that varies: results repeat bit for bit.
 //
 // The penalties, a temperature and the exponential are about 50 vector instructions a logit, beside 4 to 8 bytes of memory: 256 x 131072 fp32 with
-// histories of 8192 take 77 us, 3.5 TB/s, and with histories of 100 63 us, 4.3 TB/s.  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
+// histories of 8192 take 64.4 us, 4.2 TB/s, the vector unit 75 % busy; with histories
+// of 100 55.6 us, 4.8 TB/s.  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
 #include "common.h"
 
 #define LOGITS_COUNTS 22               // a counter's low bits: occurrences in the history; above them: the last bias entry of the token, from 1
@@ -260,14 +261,15 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsArgs a) {
 
 // Threads, logits a thread and tokens of a workgroup.  A vocabulary that one workgroup holds needs no join (256 x 9000 bf16, histories of 2000:
 // one range of 1024 threads 7.4 us, two of 512 and the join 9.9).  Else 16 logits a thread in workgroups of 512, of which a compute unit holds four
-// (256 x 131072 fp32, histories of 8192: 77 us; 32 a thread 80, 8 a thread 95; workgroups of 1024 76, but 256 x 50257 bf16 23.5 against 21.8), and 8
-// in workgroups of 256 while all of them are resident at once and shorter passes end sooner (1 x 32000: 5.8 us against 7.0; 64 x 32000 8.6 against
-// 8.7).  With rows for most compute units one workgroup also holds twice as many, 32 a thread: the join is saved and the history read once (bf16 x
-// 32000, histories of 1000: 256 rows 13.6 us against 16.0, 160 rows 12.3 against 13.2, but 128 rows 11.9 against 11.2 and one row 9.1 against 5.9).
+// (256 x 131072 fp32, histories of 8192: 76 us; 32 a thread 80, 8 a thread 95, before the stores passed the caches by; since, 64.4, and workgroups of
+// 1024 65.8, with histories of 100 55.6 and 61.4), and 8 in workgroups of 256 while all of them are resident at once and shorter passes end sooner (1 x
+// 32000: 5.8 us against 7.0; 64 x 32000 8.6 against 8.7).  Rows of up to 32768 bf16 logits for most compute units, but not more than one each: a
+// workgroup a row, 32 logits a thread, which saves the join and reads the history once (32000, histories of 1000, 160 / 192 / 224 / 256 rows: 11.1 /
+// 11.5 / 11.8 / 12.4 us against 11.9 / 12.2 / 14.1 / 14.6; but 128 rows 11.9 against 11.2, 320 rows 21.2 against 16.5; fp32 256 rows 19.9 against 16.8).
 struct LogitsPlan { int threads, each, range, ranges; };
-static LogitsPlan logits_plan(int B, int V) {
+static LogitsPlan logits_plan(int B, int V, bool bf) {
   LogitsPlan p;
-  const bool twice = V > 1024 * 16 && V <= 1024 * 32 && B >= 160, one = V <= 1024 * 16 || twice, few = !one && static_cast<long long>(B) * V <= 1 << 21;
+  const bool twice = V > 1024 * 16 && V <= 1024 * 32 && bf && B >= 160 && B <= 256, one = V <= 1024 * 16 || twice, few = !one && static_cast<long long>(B) * V <= 1 << 21;
   p.each = few ? 8 : (twice ? 32 : 16);
   p.threads = few ? 256 : (!one ? 512 : (V <= 256 * 16 ? 256 : (V <= 512 * 16 ? 512 : 1024)));
   p.ranges = (V + p.threads * p.each - 1) / (p.threads * p.each);
@@ -290,20 +292,22 @@ static hipError_t logits_launch_as(const LogitsArgs& a, hipStream_t st) {
 }
 template <typename T, typename U>
 static hipError_t logits_launch(const LogitsArgs& a, const LogitsPlan& p, hipStream_t st) {
-  if (p.each == 32) return logits_launch_as<T, U, 1024, 32>(a, st);
+  if constexpr (sizeof(T) == 2)
+    if (p.each == 32) return logits_launch_as<T, U, 1024, 32>(a, st);
   if (p.each == 8) return logits_launch_as<T, U, 256, 8>(a, st);
   return p.threads == 256 ? logits_launch_as<T, U, 256, 16>(a, st) : (p.threads == 512 ? logits_launch_as<T, U, 512, 16>(a, st) : logits_launch_as<T, U, 1024, 16>(a, st));
 }
 #define LOGITS_INSTANTIATE(T, U)                                                                                                          \
   template __global__ void logits_kernel<T, U, 256, 8>(const LogitsArgs); template __global__ void logits_kernel<T, U, 256, 16>(const LogitsArgs); \
-  template __global__ void logits_kernel<T, U, 512, 16>(const LogitsArgs); template __global__ void logits_kernel<T, U, 1024, 16>(const LogitsArgs); \
-  template __global__ void logits_kernel<T, U, 1024, 32>(const LogitsArgs);
+  template __global__ void logits_kernel<T, U, 512, 16>(const LogitsArgs); template __global__ void logits_kernel<T, U, 1024, 16>(const LogitsArgs);
 LOGITS_INSTANTIATE(bf16_t, bf16_t) LOGITS_INSTANTIATE(bf16_t, float) LOGITS_INSTANTIATE(float, bf16_t) LOGITS_INSTANTIATE(float, float)
+template __global__ void logits_kernel<bf16_t, bf16_t, 1024, 32>(const LogitsArgs);
+template __global__ void logits_kernel<bf16_t, float, 1024, 32>(const LogitsArgs);
 #undef LOGITS_INSTANTIATE
 
 extern "C" size_t ecospa_logits_workspace_bytes(int B, int V) {
   if (B < 1 || V < 1 || B > 65535 || V > (1 << 24)) return 0;
-  const LogitsPlan p = logits_plan(B, V);
+  const LogitsPlan p = logits_plan(B, V, false);      // the types are not known: the plan with more ranges
   return p.ranges > 1 ? align_up(static_cast<size_t>(B) * p.ranges * sizeof(LogitsPart), 256) : 0;
 }
 extern "C" int ecospa_logits_process(ecospa_ctx* ctx, const ecospa_logits* q) {
@@ -318,7 +322,7 @@ extern "C" int ecospa_logits_process(ecospa_ctx* ctx, const ecospa_logits* q) {
   LogitsArgs a;
   memset(&a, 0, sizeof(a));
   a.q = *q;
-  const LogitsPlan p = logits_plan(q->B, q->V);
+  const LogitsPlan p = logits_plan(q->B, q->V, q->dtype == ECOSPA_BF16);
   a.range = p.range;
   a.ranges = p.ranges;
   if (a.ranges > 1) {
