@@ -44,6 +44,7 @@ struct PrefixArgs {
   int p_tiles;             // key tiles of the prefix, as the items that read it cut it
   int p_chunks, p_chunk, p_row_tiles;      // prefix items: chunks, key tiles of a chunk, tiles of rows
   int o_chunks, o_chunk, o_row_tiles;      // own (or joint) items
+  int p_stages, o_stages;  // LDS stages that such an item comes to use (no more than its tiles of a wavefront)
   int p_items;             // prefix items in front of the others in the grid
   int own_once, prefix_once;      // keys that one item reads, too many to stay in the last cache: their loads pass the caches by
   int slots;               // pieces per row in the workspace; 0: every item is all of its rows
@@ -488,14 +489,14 @@ struct PrefixShape {
   static constexpr bool SHARE = ROWS >= ROWS_64;
   typedef std::conditional_t<ROWS >= ROWS_128, Rows32<DQ, DV, ROWS == ROWS_256 ? 2 : 1>, Rows16<DQ, DV, ROWS == ROWS_32 ? 2 : 1>> Rows;
   static constexpr int KT = SHARE ? 64 : 32, ROW_TILE = 16 << ROWS;
-  static constexpr int loop = (SHARE ? 1 : 4) * NB * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * Rows::COLS * (DV * 16 + 32) + Rows::COLS * 16) * 4;
-  static constexpr int lds = loop > join ? loop : join;
+  static constexpr int stage = (SHARE ? 1 : 4) * KT * (DQ + DV) * 2, join = SHARE ? 0 : (4 * Rows::COLS * (DV * 16 + 32) + Rows::COLS * 16) * 4;
+  static constexpr int lds(int stages) { return (stages < NB ? stages : NB) * stage > join ? (stages < NB ? stages : NB) * stage : join; }
 };
 
 // An item.  Shared tiles: the four wavefronts take their rows each.  Otherwise they share the item's rows and take the key tiles in turn, from
-// LDS buffers of their own without a barrier, and join at the end.  NB stages: NB - 1 tiles are on their way.
+// LDS buffers of their own without a barrier, and join at the end.  NB stages: NB - 1 tiles are on their way; `stages` of them are there.
 template <int DQ, int DV, int ROWS, int NB>
-__device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const lds_all) {
+__device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const lds_all, int stages) {
   typedef PrefixShape<DQ, DV, ROWS, NB> Shape;
   typedef typename Shape::Rows Rows;
   constexpr bool SHARE = Shape::SHARE;
@@ -503,7 +504,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Item it;
   if (!prefix_item<KT>(a, Shape::ROW_TILE, it)) return;
-  bf16_t* const buf = lds_all + (SHARE ? 0 : wave * NB * KT * (DQ + DV));      // [NB][K tile, V tile]
+  bf16_t* const buf = lds_all + (SHARE ? 0 : wave * stages * (KT * (DQ + DV)));      // [stages][K tile, V tile]
 
   KvLoader<DQ, KT, WAVES> kl;
   KvLoader<DV, KT, WAVES> vl;
@@ -666,16 +667,18 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
 template <int DQ, int DV, int OWN, int PREFIX>
 struct PrefixKernel {
   static constexpr int NB_S = DQ + DV <= 128 && OWN == ROWS_64 ? 3 : 2, NB_O = OWN >= ROWS_64 ? NB_S : 2, NB_P = PREFIX < ROWS_64 ? 2 : (OWN >= ROWS_64 ? NB_S : 4);
-  static constexpr int own = PrefixShape<DQ, DV, OWN, NB_O>::lds, pre = OWN == PREFIX ? 0 : PrefixShape<DQ, DV, PREFIX, NB_P>::lds;
-  static constexpr int lds = own > pre ? own : pre;
+  static constexpr int lds(int o_stages, int p_stages) {      // a call of one kind has its prefix items in o_stages too
+    const int own = PrefixShape<DQ, DV, OWN, NB_O>::lds(o_stages), pre = OWN == PREFIX ? 0 : PrefixShape<DQ, DV, PREFIX, NB_P>::lds(p_stages);
+    return own > pre ? own : pre;
+  }
 };
 // Two wavefronts a SIMD at least: the register file then has no accumulation half, and the scores need no moves between the halves.
 template <int DQ, int DV, int OWN, int PREFIX>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_attn_kernel(const PrefixArgs a) {
   typedef PrefixKernel<DQ, DV, OWN, PREFIX> K;
   extern __shared__ __attribute__((aligned(16))) bf16_t lds_all[];      // one object: see attn.hip
-  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_rows<DQ, DV, PREFIX, K::NB_P>(a, lds_all);
-  else prefix_rows<DQ, DV, OWN, K::NB_O>(a, lds_all);
+  if (OWN != PREFIX && static_cast<int>(blockIdx.x) < a.p_items) prefix_rows<DQ, DV, PREFIX, K::NB_P>(a, lds_all, min(a.p_stages, K::NB_P));
+  else prefix_rows<DQ, DV, OWN, K::NB_O>(a, lds_all, min(a.o_stages, K::NB_O));
 }
 
 // The pairs that are built: items of one kind for every width; apart, own tiles beside the prefix's for narrow heads, and shared ones for wide heads,
@@ -688,11 +691,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 constexpr bool prefix_wide(int dq, int dv) { return dq + dv > 128; }
 template <int DQ, int DV, int OWN, int PREFIX>
 static hipError_t prefix_launch(const PrefixArgs& a, unsigned grid, hipStream_t st) {
-  constexpr int lds = PrefixKernel<DQ, DV, OWN, PREFIX>::lds;
+  constexpr int most = PrefixKernel<DQ, DV, OWN, PREFIX>::lds(4, 4);
+  const int lds = PrefixKernel<DQ, DV, OWN, PREFIX>::lds(a.o_stages, a.p_stages);
   const auto kern = prefix_attn_kernel<DQ, DV, OWN, PREFIX>;
   static LdsAttrOnce attr_once;
-  if (lds > 64 * 1024) {
-    const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), lds);
+  if (most > 64 * 1024) {
+    const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), most);
     if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(kern, dim3(grid), dim3(256), lds, st, a);

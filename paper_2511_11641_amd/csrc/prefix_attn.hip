@@ -209,8 +209,21 @@ static double join_cost(const PrefixArgs& a, int slots) {
 }
 static inline long long ceil_div(long long x, long long y) { return (x + y - 1) / y; }
 
+// LDS of an item whose wavefronts take `steps` tiles each, as PrefixShape has it (an upper bound on the stages will do).
+static int lds_of(const PrefixPlan& p, int kind, long long steps, int stages) {
+  return static_cast<int>(steps < stages ? (steps > 0 ? steps : 1) : stages) * keys_of(kind) * tiles_at_once(kind) * (p.dq + p.dv) * 2;
+}
+// Workgroups at work at once, by LDS and by the registers of their kind.  Items of a single step hold one stage, which leaves room for twice as many (60
+// x 4 tokens on 4 own keys, 16 heads of 128 + 128 dims, 15.8 -> 9.8 us; 89 tokens on 49 + 1 keys, 32 heads of 48 + 48 dims, 23.9 -> 16.4).
+static long long resident_of(const PrefixPlan& p, int kind, int lds) {
+  const int dims = p.dq + p.dv, by_lds = lds > 0 ? 160 * 1024 / lds : 4;
+  const int by_regs = kind == ROWS_256 ? 2 : (kind == ROWS_128 ? (dims <= 64 ? 4 : (dims <= 128 ? 3 : 2)) : (dims <= 128 ? 4 : (kind == ROWS_32 ? 2 : 3)));
+  const int n = by_lds < by_regs ? by_lds : by_regs;
+  return 256ll * (n > 0 ? n : 1);
+}
+
 // Items that run over the prefix and then the own keys of their request: `chunks` of them per tile of rows.
-static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool set) {
+static double plan_joint(PrefixArgs& a, PrefixPlan& p, bool set) {
   const int kt = keys_of(p.own), at_once = tiles_at_once(p.own);
   const long long pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles;
   const long long tiles = ceil_div(a.P, kt) + ceil_div(a.own_max, kt), steps = ceil_div(tiles, at_once);
@@ -218,6 +231,7 @@ static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
   long long best_chunk = 0;
   for (long long chunks = 1; chunks <= 64 && (chunks == 1 || ceil_div(steps, chunks) >= 2); chunks += (chunks < 8 ? 1 : chunks / 4)) {
     const long long chunk = steps > 0 ? ceil_div(steps, chunks) : 1, n = steps > 0 ? ceil_div(steps, chunk) : 1, wgs = pairs * n;
+    const long long resident = resident_of(p, p.own, lds_of(p, p.own, chunk, 2));
     const double active = static_cast<double>(wgs < resident ? wgs : resident), rounds = wgs <= resident ? 1 : static_cast<double>(wgs) / resident + 0.15;
     const ItemCost c = item_cost(a, p, p.own, static_cast<double>(chunk), static_cast<double>(a.P + a.own_max) / n, active, active, a.o_row_tiles);
     const double cost = rounds * c.item + join_cost(a, static_cast<int>(n));
@@ -231,11 +245,12 @@ static double plan_joint(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
     a.o_chunk = static_cast<int>(best_chunk * at_once);
     a.o_chunks = tiles > 0 ? static_cast<int>(ceil_div(tiles, a.o_chunk)) : 1;
     a.slots = a.o_chunks > 1 ? a.o_chunks : 0;
+    a.o_stages = a.p_stages = static_cast<int>(best_chunk < 4 ? best_chunk : 4);
   }
   return best;
 }
 // Items of the prefix for the rows of all requests, and items of own keys.
-static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool set) {
+static double plan_apart(PrefixArgs& a, PrefixPlan& p, bool set) {
   const int prefix = kind_of(a.rows) < p.own ? p.own : kind_of(a.rows), kt_p = keys_of(prefix), at_once_p = tiles_at_once(prefix);
   const int kt = keys_of(p.own), at_once = tiles_at_once(p.own);
   const long long row_tiles = ceil_div(a.rows, rows_of(prefix)), pairs = static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles;
@@ -247,6 +262,8 @@ static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
       const long long p_chunk = ceil_div(p_steps, pc), o_chunk = o_steps > 0 ? ceil_div(o_steps, oc) : 1;
       const long long p_n = ceil_div(p_steps, p_chunk), o_n = ceil_div(o_steps, o_chunk);
       const double p_wgs = static_cast<double>(a.h_kv * row_tiles * p_n), o_wgs = static_cast<double>(pairs * o_n), wgs = p_wgs + o_wgs;
+      const int lds_p = lds_of(p, prefix, p_chunk, prefix >= ROWS_64 && p.own < ROWS_64 ? 4 : 2), lds_o = lds_of(p, p.own, o_chunk, 2);
+      const long long resident = resident_of(p, prefix, lds_p > lds_o ? lds_p : lds_o);
       const double active = wgs < resident ? wgs : static_cast<double>(resident);
       const double p_keys = static_cast<double>(a.P) / p_n, o_keys = static_cast<double>(a.own_max) / (o_n > 0 ? o_n : 1);
       const ItemCost cp = item_cost(a, p, prefix, static_cast<double>(p_chunk), p_keys, active, active * p_wgs / wgs, static_cast<double>(row_tiles));
@@ -266,6 +283,9 @@ static double plan_apart(PrefixArgs& a, PrefixPlan& p, long long resident, bool 
     a.o_chunk = static_cast<int>(best_o * at_once);
     a.o_chunks = static_cast<int>(ceil_div(ceil_div(a.own_max, kt), a.o_chunk));
     a.slots = a.p_chunks + a.o_chunks;
+    a.p_stages = static_cast<int>(best_p < 4 ? best_p : 4);
+    a.o_stages = static_cast<int>(best_o < 4 ? best_o : 4);
+    if (prefix == p.own && a.o_stages < a.p_stages) a.o_stages = a.p_stages;
   }
   return best;
 }
@@ -278,30 +298,25 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   a.o_row_tiles = static_cast<int>(ceil_div(a.own_rows, rows_of(p.own)));
   const long long rows = static_cast<long long>(a.h_kv) * a.rows;
   if (static_cast<long long>(a.B) * a.h_kv * a.o_row_tiles * 64 > 0x7fffffffll || rows * 128 > 0x7fffffffll * 64) return false;
-  // workgroups that fit at once: by the LDS of own tiles (512 bytes a dim), or of shared ones with two stages (256) and their registers
-  const int lds = 512 * (p.dq + p.dv);
-  const long long resident_own = 256ll * (lds <= 40960 ? 4 : (lds <= 53248 ? 3 : (lds <= 81920 ? 2 : 1)));
-  const long long resident_128 = 256ll * (p.dq + p.dv <= 64 ? 4 : (p.dq + p.dv <= 128 ? 3 : 2));
-  const long long resident_joint = p.own >= ROWS_64 ? resident_128 : resident_own;
   // Rows of a request that fill a tile of their own, a batch of one or no prefix: nothing to gain by putting requests together.
   const bool only_joint = a.B == 1 || a.P == 0 || p.own >= ROWS_64;
   // Wide heads apart: own tiles for every wavefront take so much LDS that one workgroup is left to a compute unit; shared tiles leave two, and a
   // wavefront with the few rows keeps up with memory (12 x 5 tokens on 8191, 96 and 128 dims: 49 -> 44 us; 64 and 64 dims: no difference).
   const int own = p.own, apart_own = prefix_wide(p.dq, p.dv) ? ROWS_64 : p.own;
-  const double joint = only_joint ? 0 : plan_joint(a, p, resident_joint, false);
+  const double joint = only_joint ? 0 : plan_joint(a, p, false);
   p.own = apart_own;
-  if (!only_joint && plan_apart(a, p, apart_own == ROWS_64 ? resident_128 : resident_own, false) < joint) {
-    plan_apart(a, p, apart_own == ROWS_64 ? resident_128 : resident_own, true);
+  if (!only_joint && plan_apart(a, p, false) < joint) {
+    plan_apart(a, p, true);
   } else {
     p.own = own;
-    plan_joint(a, p, resident_joint, true);
+    plan_joint(a, p, true);
     // Prompts: 64 rows a wavefront halve the reads of LDS, where narrow heads leave the registers and there are workgroups enough for two on every
     // compute unit several times over (16 x 509 tokens on 8192, 4 query heads a key/value head: 653 -> 618 us; 8 x 256 on 2048 with its half as
     // many workgroups: 43 -> 48).
     if (own == ROWS_128 && !prefix_wide(p.dq, p.dv) && a.slots == 0 && static_cast<long long>(a.B) * a.h_kv * ceil_div(a.own_rows, 256) >= 1024) {
       p.own = ROWS_256;
       a.o_row_tiles = static_cast<int>(ceil_div(a.own_rows, 256));
-      plan_joint(a, p, 512, true);
+      plan_joint(a, p, true);
     }
   }
   // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call: their loads pass the caches by.  Own
@@ -312,6 +327,8 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   a.prefix_once = once(a.h_kv, a.P, a.joint ? a.B * a.o_row_tiles : a.p_row_tiles);
   // the kernels cut the keys as the plan did
   if (a.p_tiles != ceil_div(a.P, keys_of(p.prefix)) || p.prefix < p.own) return false;
+  const auto held = [](int stages, int chunk, int kind) { return stages >= 4 || ceil_div(chunk, tiles_at_once(kind)) <= stages; };
+  if (!held(a.o_stages, a.o_chunk, p.own) || !held(p.prefix == p.own ? a.o_stages : a.p_stages, a.p_chunk, p.prefix)) return false;
   // The weights need every own score against a sum that is complete only at the end.  Kept scores are written and read, 8 bytes a row and key;
   // without them the keys are read a second time, 2 kp_qk bytes a key, in a launch of its own.
   const bool keep = weights && a.own_rows <= 32 && a.own_max > 0 && 4 * a.own_rows <= a.kq;
