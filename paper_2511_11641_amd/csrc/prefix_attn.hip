@@ -120,57 +120,84 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
 }
 
 // ---------------------------------------------------------------------------------------------
-// Weights: w_out[j] = w_in[j] + sum over the rows of the request that see own key j of exp(s_j - lse).  A wavefront takes 32 keys: their fragments
-// stay in registers while the rows pass by, 16 at a time; the sum over a tile's rows is a sum over lanes.  Bound like the scores' part of the
-// attention, at half its products; taken where keeping scores would move more (many rows a request: prompts).
+// Weights: w_out[j] = w_in[j] + sum over the rows of the request that see own key j of exp(s_j - lse).  Keys stay in registers while the rows pass by from
+// the first that sees a key, 32 at a time, the next ones on their way; S^T = K Q^T, so that the sum over rows is a sum over lanes, taken once at the end.
+// MANY rows: 64 keys a workgroup, its wavefronts take the rows in turn.  Otherwise 32 keys a wavefront, and no key is read twice.  Bound by the latency
+// of the rows' reads, then by the exponentials: 16 x 509 tokens of 32 heads on their own 509 keys 36 us, the attention itself 611.
 // ---------------------------------------------------------------------------------------------
-template <int DQ>
-__global__ __launch_bounds__(256) void prefix_weights_kernel(const PrefixArgs a, const float* lse, const float* w_in, float* w_out, int cap) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), grp = lane >> 4, l16 = lane & 15;
+template <int DQ, bool MANY>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_weights_kernel(const PrefixArgs a, const float* lse, const float* w_in,
+                                                                                                     float* w_out, int cap) {
+  constexpr int KT = MANY ? 2 : 1, STEP = MANY ? 128 : 32;      // tiles of 32 keys; rows from one of a wavefront's tiles to its next
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hh = lane >> 5, l32 = lane & 31;
   const int b = blockIdx.y / a.h_kv, hk = blockIdx.y - b * a.h_kv;
-  const int n = own_len(a, b), k0 = (blockIdx.x * 4 + wave) * 32;
+  const int n = own_len(a, b), k0 = MANY ? blockIdx.x * 64 : (blockIdx.x * 4 + wave) * 32;
   if (k0 >= n) return;
   const bf16_t* const kb = a.k + b * a.k_sb + hk * a.k_sh;
-  bf16x8_t kf[2][DQ / 32];
+  bf16x8_t kf[KT][DQ / 16];
 #pragma unroll
-  for (int t = 0; t < 2; ++t)
+  for (int u = 0; u < KT; ++u)
 #pragma unroll
-    for (int i = 0; i < DQ / 32; ++i)
-      kf[t][i] = *reinterpret_cast<const bf16x8_t*>(kb + min(k0 + 16 * t + l16, n - 1) * a.k_st + min(32 * i + 8 * grp, a.kq - 8));
-  float sum[2][4] = {};
-  for (int r0 = 0; r0 < a.own_rows; r0 += 16) {
-    const int r = min(r0 + l16, a.own_rows - 1), t = r / a.g, head = hk * a.g + (r - t * a.g);
-    const long long token = static_cast<long long>(b) * a.L + t;
-    const bf16_t* const src = a.q + token * a.ld_q + static_cast<long long>(head) * a.kq;
-    bf16x8_t qf[DQ / 32];
+    for (int c = 0; c < DQ / 16; ++c)
+      kf[u][c] = *reinterpret_cast<const bf16x8_t*>(kb + min(k0 + 32 * u + l32, n - 1) * a.k_st + min(16 * c + 8 * hh, a.kq - 8));
+  const int first = max(k0 - (n - a.L), 0) * a.g;      // the first token that sees key k0
+  const int start = first + (MANY ? 32 * wave : 0) + l32, step_t = STEP / a.g, step_i = STEP - step_t * a.g;
+  int t = start / a.g, i = start - t * a.g;      // the lane's row: token and query head of the group
+  const auto load = [&](u32x4 (&x)[DQ / 16], float& ref) __attribute__((always_inline)) {      // rows behind the last: the last one
+    const int head = hk * a.g + (t < a.L ? i : a.g - 1), tt = min(t, a.L - 1);
+    const bf16_t* const src = a.q + (static_cast<long long>(b) * a.L + tt) * a.ld_q + static_cast<long long>(head) * a.kq;
 #pragma unroll
-    for (int i = 0; i < DQ / 32; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(src + min(32 * i + 8 * grp, a.kq - 8));
-      qf[i] = __builtin_bit_cast(bf16x8_t, 32 * i + 8 * grp < a.kq ? x : u32x4{0u, 0u, 0u, 0u});
-    }
-    const float ref = lse[(static_cast<long long>(b) * a.h + head) * a.L + t] * LOG2E;
-    const int left = (r0 + l16 < a.own_rows ? own_visible(n, a.L, t) : 0) - k0 - 4 * grp;
+    for (int c = 0; c < DQ / 16; ++c) x[c] = *reinterpret_cast<const u32x4*>(src + min(16 * c + 8 * hh, a.kq - 8));
+    ref = lse[(static_cast<long long>(b) * a.h + head) * a.L + tt];
+  };
+  float sum[KT][16] = {};
+  u32x4 next[DQ / 16];
+  float next_ref;
+  load(next, next_ref);
+  for (int r0 = start - l32; r0 < a.own_rows; r0 += STEP) {
+    bf16x8_t qf[DQ / 16];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      floatx4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < DQ / 16; ++c) qf[c] = __builtin_bit_cast(bf16x8_t, 16 * c + 8 * hh < a.kq ? next[c] : u32x4{0u, 0u, 0u, 0u});
+    const float ref = next_ref * LOG2E;
+    const int left = (t < a.L ? own_visible(n, a.L, t) : 0) - k0;      // keys from k0 on that the row sees
+    t += step_t;
+    i += step_i;
+    while (i >= a.g) { i -= a.g; ++t; }
+    if (r0 + STEP < a.own_rows) load(next, next_ref);
+    const bool whole = __builtin_amdgcn_ballot_w64(left < 32 * KT) == 0ull;
 #pragma unroll
-      for (int i = 0; i < DQ / 32; ++i) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u][i], qf[i], s, 0, 0, 0);
+    for (int u = 0; u < KT; ++u) {
+      floatx16 s = {};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int c = 0; c < DQ / 16; ++c) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][c], qf[c], s, 0, 0, 0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.sc, -ref));
-        sum[u][e] += 16 * u + e < left ? p : 0.f;
+        sum[u][e] += whole || 32 * u + 8 * (e / 4) + 4 * hh + e % 4 < left ? p : 0.f;
       }
     }
   }
+  float total = 0.f;      // without MANY: lane e of either half keeps the sum of register e
+  __shared__ float all[4][32 * KT];
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+  for (int u = 0; u < KT; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < 16; ++e) {
       const float x = row16_sum(sum[u][e]);
-      const int j = k0 + 16 * u + 4 * grp + e;
-      const long long at = static_cast<long long>(blockIdx.y) * cap + j;
-      if (l16 == 0 && j < n) w_out[at] = (w_in ? w_in[at] : 0.f) + x;
+      const float y = x + __shfl_xor(x, 16);
+      if (!MANY) total = l32 == e ? y : total;
+      else if (l32 == 0) all[wave][32 * u + 8 * (e / 4) + 4 * hh + e % 4] = y;
     }
+  int j = k0 + 8 * (l32 / 4) + 4 * hh + l32 % 4;
+  bool writes = l32 < 16;
+  if constexpr (MANY) {
+    __syncthreads();
+    j = k0 + lane;
+    writes = wave == 0;
+    total = (all[0][lane] + all[1][lane]) + (all[2][lane] + all[3][lane]);
+  }
+  const long long at = static_cast<long long>(blockIdx.y) * cap + j;
+  if (writes && j < n) w_out[at] = (w_in ? w_in[at] : 0.f) + total;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -188,24 +215,28 @@ struct PrefixPlan {
   size_t part_o, part_ml, lse, scores;      // bytes of workspace
 };
 
-// What the items of a call cost, in ns, for the choice between ways to cut it.  Constants as measured: an item's start and end 3 us, a step's least
-// time (a latency of memory, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5 bytes/ps of memory over
-// all workgroups (`share` of them read the same keys), and a row and key of a tile on a compute unit (heads of 64 + 64 dims 0.08 ns; the unused rows
-// of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them such items.  Chunks of the prefix forced to other counts
-// (8 to 48, 1 and 2 of own keys): the choice is within 1 % of the best for 64 requests on 32768 tokens (15 chosen, 12 best; with weights 81 us
-// against 77), for 12 x 5 on 8191 and 8 on 2000 the best, for 32 on 4096 21.0 us against 19.4 (6 chosen, 3 best).
+// What the items of a call cost, in ns, for the choice between ways to cut it.  Constants as measured: an item's start and end 3 us, a step's least time (a
+// latency of memory and what a compute unit can take in, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5
+// bytes/ps of memory over all workgroups (`share` of them read the same keys), and a row and key of a tile on a compute unit (heads of 64 + 64 dims 0.08
+// ns; the unused rows of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them such items.  Chunks of the prefix forced to
+// other counts (8 to 48, 1 and 2 of own keys): the choice is within 1 % of the best for 64 requests on 32768 tokens (15 chosen, 12 best; with weights 81 us
+// against 77), for 12 x 5 on 8191 and 8 on 2000 the best, for 32 on 4096 21.0 us against 19.4 (6 chosen, 3 best).  Over 200 random shapes, joint items or
+// items apart forced, the choice lost 1.4 % in the mean against the better one, 39 % at most (16.4 us against 11.8); the join's 4 us and the 7 ns a dim of
+// a step, set after that, took 0.3 % off 600 shapes (0.67 to 1.075 of the time each).
 struct ItemCost { double step, item; };
 static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double keys, double active, double alike, double share) {
   const double per_cu = std::ceil(alike / 256), step_keys = keys_of(kind) * tiles_at_once(kind);
   const double pair = (0.02 + 0.0005 * (p.dq + p.dv)) * (kind == ROWS_256 ? 0.92 : 1);
-  const double memory = active * (keys < step_keys ? keys : step_keys) * (a.kq + a.kv) * 2 / (5500 * share), compute = per_cu * rows_of(kind) * step_keys * pair;
-  double step = kind >= ROWS_64 ? (kind == ROWS_64 ? 0.7 : (kind == ROWS_128 ? 1 : 1.7)) * (600 + 6 * (p.dq + p.dv)) : 900;      // a wavefront by itself
+  const double memory = active * (keys < step_keys ? keys : step_keys) * (a.kq + a.kv) * 2 / (5500 * share);
+  const double compute = per_cu * rows_of(kind) * step_keys * pair;
+  const double of_kind = kind == ROWS_64 ? 0.7 : (kind == ROWS_128 ? 1 : 1.7);
+  double step = kind >= ROWS_64 ? of_kind * (600 + 6 * (p.dq + p.dv)) : std::fmax(700, 7 * (a.kq + a.kv));      // a wavefront by itself
   if (memory > step) step = memory;
   if (compute > step) step = compute;
   return {step, 3000 + steps * step};
 }
 static double join_cost(const PrefixArgs& a, int slots) {
-  return slots > 1 ? 3000 + static_cast<double>(a.h_kv) * a.rows * slots * (a.kv + 2) * 8 / 5000 : 0;
+  return slots > 1 ? 4000 + static_cast<double>(a.h_kv) * a.rows * slots * (a.kv + 2) * 8 / 5000 : 0;
 }
 static inline long long ceil_div(long long x, long long y) { return (x + y - 1) / y; }
 
@@ -361,9 +392,12 @@ static void prefix_join_launch(const PrefixArgs& a, const PrefixPlan& p, hipStre
   const auto kern = few ? prefix_join_kernel<W, true> : prefix_join_kernel<W, false>;
   hipLaunchKernelGGL(kern, dim3(blocks + p.weigh), dim3(256), 0, st, a, keys_of(p.own), rows_of(p.own), blocks);
 }
-template __global__ void prefix_weights_kernel<32>(const PrefixArgs, const float*, const float*, float*, int);
-template __global__ void prefix_weights_kernel<64>(const PrefixArgs, const float*, const float*, float*, int);
-template __global__ void prefix_weights_kernel<128>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<32, false>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<32, true>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<64, false>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<64, true>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<128, false>(const PrefixArgs, const float*, const float*, float*, int);
+template __global__ void prefix_weights_kernel<128, true>(const PrefixArgs, const float*, const float*, float*, int);
 
 int ecospa_cache_check(const ecospa_cache* c) {
   if (!c || !c->k || !c->v || !c->lens || (c->P > 0 && (!c->pk || !c->pv))) return ECOSPA_ERR_NULL;
@@ -445,8 +479,13 @@ extern "C" int ecospa_prefix_attn(ecospa_ctx* ctx, const ecospa_cache* cache, in
     ECOSPA_CHECK_LAUNCH(ctx, "prefix_join_kernel");
   }
   if (p.lse && a.own_max > 0) {
-    const dim3 grid((a.own_max + 127) / 128, a.B * a.h_kv);
-    const auto kern = p.dq == 32 ? prefix_weights_kernel<32> : (p.dq == 64 ? prefix_weights_kernel<64> : prefix_weights_kernel<128>);
+    // whole calls, MANY against not: 512 rows (8 x 8 heads, 128 tokens) 20.0 us / 24.1, 2048 rows 58.8 / 76.1, 512 rows of single heads 108.3 / 108.5; but
+    // 256 rows of single heads 40.2 / 30.4 and 33 rows 25.9 / 18.1
+    const bool many = a.own_rows >= 512;
+    const dim3 grid((a.own_max + (many ? 63 : 127)) / (many ? 64 : 128), a.B * a.h_kv);
+    const auto few_kern = p.dq == 32 ? prefix_weights_kernel<32, false> : (p.dq == 64 ? prefix_weights_kernel<64, false> : prefix_weights_kernel<128, false>);
+    const auto many_kern = p.dq == 32 ? prefix_weights_kernel<32, true> : (p.dq == 64 ? prefix_weights_kernel<64, true> : prefix_weights_kernel<128, true>);
+    const auto kern = many ? many_kern : few_kern;
     hipLaunchKernelGGL(kern, grid, dim3(256), 0, ctx->stream, a, lse, weights_in, weights_out, cache->cap);
     ECOSPA_CHECK_LAUNCH(ctx, "prefix_weights_kernel");
   }

@@ -84,7 +84,7 @@ LENGTHS = [
     (1, 1, 4, 4, 0, [1]), (1, 1, 4, 4, 0, [0]), (1, 1, 4, 2, 1, [0]), (1, 1, 6, 6, 61, [33]),
     (3, 1, 4, 4, 64, [0, 1, 65]), (3, 1, 4, 4, 63, [64, 63, 128]), (5, 1, 8, 1, 65, [31, 32, 33, 95, 97]), (2, 1, 32, 1, 130, [7, 260]),
     (4, 3, 4, 2, 0, [3, 1, 0, 70]), (2, 5, 6, 3, 129, [5, 66]), (3, 8, 8, 2, 40, [8, 40, 2]), (2, 40, 4, 2, 33, [40, 100]), (1, 70, 6, 2, 300, [170]),
-    (2, 130, 4, 4, 0, [130, 129]), (40, 1, 4, 2, 700, [1 + 13 * i % 97 for i in range(40)]), (9, 1, 16, 4, 2100, [1 + 301 * i % 1300 for i in range(9)]),
+    (2, 130, 4, 4, 0, [130, 129]), (3, 140, 12, 3, 20, [200, 140, 139]), (2, 97, 40, 1, 0, [97, 300]), (2, 15, 70, 2, 9, [15, 14]), (40, 1, 4, 2, 700, [1 + 13 * i % 97 for i in range(40)]), (9, 1, 16, 4, 2100, [1 + 301 * i % 1300 for i in range(9)]),
     (1, 1, 8, 8, 9000, [200]), (1, 2, 4, 4, 0, [20000]), (24, 2, 12, 3, 5000, [2 + 37 * i % 500 for i in range(24)]),
 ]
 
