@@ -19,6 +19,9 @@
 // of its score, and maximum, scaling, sum and conversion as long again - 256 rows x 8 heads on 32768 keys 41 us, 417 TFLOP/s with its join; 16 x 509 tokens on 8192 keys 612 us, 950 TFLOP/s, at the clock that
 // power allows (1.9 GHz).  Both at once, 64 requests on 32768 + 2048 keys: 71 us.  A single short request, latency: 61 + 33 keys 4.5 us.
 //
+// Only a row that sees no key has a sum of exponentials of zero; it is told by that.  A row that meets a score that is not a number, or +inf, has a sum,
+// an output, a log-sum-exp and weights that are not numbers, in whatever piece the key lies (its maximum may say -inf: maxima pass over NaN).
+//
 // Rounding: scores, maxima, sums and accumulators are fp32; the probabilities enter the second product rounded to bf16 (the matrix
 // unit's type), the denominator is summed from the unrounded ones, so that lse and the weights keep fp32 accuracy.
 #pragma once
@@ -463,7 +466,7 @@ __device__ __forceinline__ floatx4 prefix_weights_before(const PrefixArgs& a, lo
   return w;
 }
 // Accumulated weights of own keys j .. j + 3 (those below n) of request and head bh, from the kept scores of its rows: w_out = w_in + sum over the rows of
-// exp2(score - lse2).  early: prefix_scores() of rows 0 .. 3, before: prefix_weights_before(), both asked for in front of what lse2 waits for.
+// exp2(score - lse2), nothing where the score is -inf (the row does not see the key, whatever its lse2 is).  early: prefix_scores() of rows 0 .. 3, before: prefix_weights_before(), both asked for in front of what lse2 waits for.
 __device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, PrefixScores early, const floatx4& before, const float* lse2, int n, int j) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
   for (int r = 0; r < a.own_rows; r += 4) {
@@ -472,7 +475,7 @@ __device__ __forceinline__ void prefix_weigh(const PrefixArgs& a, long long bh, 
     for (int i = 0; i < 4; ++i) {
       const float ref = r + i < a.own_rows ? lse2[r + i] : INFINITY;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum[e] += __builtin_amdgcn_exp2f(early.x[i][e] - ref);
+      for (int e = 0; e < 4; ++e) sum[e] += early.x[i][e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(early.x[i][e] - ref);
     }
   }
 #pragma unroll
@@ -587,7 +590,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
     if (a.slots == 0) {
       const int token = row / a.g, head = it.hk * a.g + (row - token * a.g);
       if (d < a.kv) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         floatx4 f;
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = acc[i] * inv;
@@ -595,7 +598,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
       }
       if (q == 0 && a.lse && Rows::lead()) {
         const int b = token / a.L;
-        a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l > 0.f ? (m * a.sc + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+        a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l == 0.f ? -INFINITY : (m * a.sc + __builtin_amdgcn_logf(l)) * LN2;
       }
     } else {
       const long long at = (static_cast<long long>(it.hk) * a.rows + row) * a.slots + it.slot;
@@ -650,7 +653,7 @@ __device__ __forceinline__ void prefix_rows(const PrefixArgs& a, bf16_t* const l
         }
         write(c, u, f, m_all, l_all);
       }
-      if (a.slots == 0 && wave == 0 && Rows::lead()) lse2[c * 16 + l16] = l_all > 0.f ? m_all * a.sc + __builtin_amdgcn_logf(l_all) : INFINITY;
+      if (a.slots == 0 && wave == 0 && Rows::lead()) lse2[c * 16 + l16] = l_all == 0.f ? INFINITY : m_all * a.sc + __builtin_amdgcn_logf(l_all);
     }
     if (a.slots == 0 && keep) {      // the item has seen all of its rows' keys: weights from the scores it kept
       __threadfence_block();

@@ -39,7 +39,7 @@ __device__ void prefix_join_weights(const PrefixArgs& a, int kt, int row_tile, l
     }
     const float top = wave_max(m), ref = top == -INFINITY ? 0.f : top;
     l = wave_sum(l * __builtin_amdgcn_exp2f(m - ref));
-    if (lane == 0) lse2[r] = l > 0.f ? ref + __builtin_amdgcn_logf(l) : INFINITY;
+    if (lane == 0) lse2[r] = l == 0.f ? INFINITY : ref + __builtin_amdgcn_logf(l);
   }
   __syncthreads();
   if (key < n) prefix_weigh(a, bh, early, before, lse2, n, key);
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
     float top = m;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {      // slots that no item wrote hold anything
-      x[j].x = i0 + j * GROUPS < n ? x[j].x : -INFINITY;
+      if (i0 + j * GROUPS >= n) x[j] = float2{-INFINITY, 0.f};
       top = fmaxf(top, x[j].x);
     }
     const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(m - ref);
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
     for (int e = 0; e < 4; ++e) o[e] *= f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (x[j].x == -INFINITY) continue;
+      if (x[j].y == 0.f) continue;      // no key seen; not by the maximum, which is -inf where all scores are NaN too
       const float w = __builtin_amdgcn_exp2f(x[j].x - ref);
       l += w * x[j].y;
 #pragma unroll
@@ -110,13 +110,13 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
     }
   }
   if (lane * 4 < a.kv) {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] *= inv;
     *reinterpret_cast<bf16x4_t*>(a.o + token * a.ld_o + static_cast<long long>(head) * a.kv + d) = __builtin_convertvector(o, bf16x4_t);
   }
   if (lane == 0 && a.lse)
-    a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * LN2 : -INFINITY;
+    a.lse[(static_cast<long long>(b) * a.h + head) * a.L + (token - b * a.L)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2;
 }
 
 // ---------------------------------------------------------------------------------------------
