@@ -122,6 +122,6 @@ def logits_process(x, history=None, history_len=None, repetition=None, frequency
         if top > -np.inf:
             pick[b] = int(np.flatnonzero(ok & (x[b] == top))[0])
             lse[b] = np.inf if top == np.inf else top + np.log(np.exp(x[b] - top).sum())
-        elif not ok.all():
+        if not ok.all():                                   # a sum with what is not a number in it, whatever else there is
             lse[b] = np.nan
     return x, pick, lse

@@ -38,7 +38,7 @@ __device__ __forceinline__ float logits_div(float x, float d, float r) {
 }
 __device__ __forceinline__ void logits_finish(const LogitsArgs& a, int b, float m, float s, int at) {
   if (a.q.pick) a.q.pick[b] = at;
-  if (a.q.lse) a.q.lse[b] = m == INFINITY ? INFINITY : (m == -INFINITY ? 0.f : m) + logf(s);
+  if (a.q.lse) a.q.lse[b] = (m == -INFINITY ? 0.f : m) + logf(s);
 }
 
 // Eight wavefronts a SIMD with 16 logits a thread: left to itself the compiler takes 4 registers more than they have (256 x 131072 fp32 77 -> 72 us).
@@ -213,7 +213,8 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(EACH ==
   m = red_m[0];
 #pragma unroll
   for (int w = 1; w < WAVES; ++w) m = fmaxf(m, red_m[w]);
-  const float ref = m == -INFINITY ? 0.f : m;
+  // against +inf nothing could be told from what is not a number: the largest finite value in its place makes a sum of +inf, or NaN beside a NaN
+  const float ref = m == -INFINITY ? 0.f : fminf(m, 3.402823466e38f);
   float s = 0.f;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c)
