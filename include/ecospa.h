@@ -567,7 +567,9 @@ int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src /*host*/, const 
  * out (dtype out_dtype, may be the logits themselves with the same type and ld; NULL: not wanted) receives x rounded once, pick
  * (int32[B], NULL: not wanted) the lowest token with the largest x before rounding (NaN ranks below every number; -1: every token
  * is -inf or NaN) and lse (float[B], NULL: not wanted) log sum exp x (NaN where any x is NaN, else +inf where any x is).  Each of the
- * parameter arrays may be NULL (1 for repetition and temperature, 0 for the others).  dtype ECOSPA_F32 or ECOSPA_BF16, fp32 arithmetic.
+ * parameter arrays may be NULL (1 for repetition and temperature, 0 for the others).  Quotients are a division's, by zero too: a
+ * temperature of 0 makes logits infinities of their sign (0: NaN), and the pick the first positive one; the largest logit is the pick
+ * of any positive temperature.  dtype ECOSPA_F32 or ECOSPA_BF16, fp32 arithmetic.
  * Errors: ERR_NULL; ERR_DTYPE; ERR_SHAPE (B, V < 1, B > 65535, V > 2^24, leading dimensions, n_bias outside [0, 1023], history rows
  * of 2^22 entries and more); ERR_ALIGN (logits, out: 16 bytes, leading dimensions % 8); ERR_WORKSPACE
  * (ecospa_logits_workspace_bytes). */

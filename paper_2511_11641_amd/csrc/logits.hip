@@ -11,6 +11,8 @@
 // of 100 55.6 us, 4.8 TB/s.  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
 #include "common.h"
 
+#include <type_traits>
+
 #define LOGITS_COUNTS 22               // a counter's low bits: occurrences in the history; above them: the last bias entry of the token, from 1
 #define LOGITS_MAX_BIAS 1023
 
@@ -31,10 +33,22 @@ struct LogitsArgs {
 };
 
 // x / d for a divisor whose rounded reciprocal r is at hand: the product with it and one correction by its exact remainder, half the
-// division's instructions (which are what bounds these kernels beside memory); infinities keep the plain product.
-__device__ __forceinline__ float logits_div(float x, float d, float r) {
-  const float y = x * r, e = __builtin_fmaf(-y, d, x);
-  return __builtin_fmaf(fabsf(e) < INFINITY ? e : 0.f, r, y);
+// division's instructions (which are what bounds these kernels beside memory); infinite x keep the plain product.  plain: d and r are finite, as nearly
+// always.  Otherwise (plain is false) nothing is corrected where the remainder is no number, and a subnormal d, which can lack a finite reciprocal,
+// is taken 2^64 times as large, the quotient after it.
+struct LogitsDivisor {
+  float d, r, after;
+  bool plain;
+};
+__device__ __forceinline__ LogitsDivisor logits_divisor(float d) {
+  const float after = fabsf(d) < 1.17549435e-38f ? 18446744073709551616.f : 1.f, r = 1.f / (d * after);
+  return {d * after, r, after, after == 1.f && fabsf(d) < INFINITY};
+}
+template <bool PLAIN>
+__device__ __forceinline__ float logits_div(float x, const LogitsDivisor& by) {
+  const float y = x * by.r, e = __builtin_fmaf(-y, by.d, x);
+  if (PLAIN) return __builtin_fmaf(fabsf(e) < INFINITY ? e : 0.f, by.r, y);
+  return (fabsf(e) < INFINITY ? __builtin_fmaf(e, by.r, y) : y) * by.after;
 }
 __device__ __forceinline__ void logits_finish(const LogitsArgs& a, int b, float m, float s, int at) {
   if (a.q.pick) a.q.pick[b] = at;
@@ -70,7 +84,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(EACH ==
 #pragma unroll
   for (int e = 0; e < EARLY; ++e) id[e] = hist > 0 ? h[min(e * THREADS + tid, hist - 1)] : -1;
   const float rep = q.repetition ? q.repetition[b] : 1.f, freq = q.frequency ? q.frequency[b] : 0.f, pres = q.presence ? q.presence[b] : 0.f;
-  const float temp = q.temperature ? q.temperature[b] : 1.f, rep_r = 1.f / rep, temp_r = 1.f / temp;
+  const LogitsDivisor by_rep = logits_divisor(rep), by_temp = logits_divisor(q.temperature ? q.temperature[b] : 1.f);
   const int mr = q.mask ? q.mask_row[b] : -1;
   const unsigned* const mask = mr >= 0 && mr < q.n_masks ? q.mask + mr * q.ld_mask : nullptr;
   unsigned allowed[CHUNKS];
@@ -152,16 +166,25 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(EACH ==
       *reinterpret_cast<int4*>(k + 4) = *reinterpret_cast<const int4*>(count + i + 4);
       if (k[0] | k[1] | k[2] | k[3] | k[4] | k[5] | k[6] | k[7]) {
         unsigned entries = 0u;
+        const auto penalise = [&](auto plain) __attribute__((always_inline)) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {      // without branches: among 512 tokens of a wavefront some are in any history
-          const int past = k[e] & ((1 << LOGITS_COUNTS) - 1);
-          entries |= static_cast<unsigned>(k[e]);
-          const bool up = x[c][e] > 0.f;      // x / rep as logits_div(), otherwise x rep
-          const float f = up ? rep_r : rep, y0 = x[c][e] * f, r0 = __builtin_fmaf(-y0, rep, x[c][e]);
-          const float y = __builtin_fmaf(up && fabsf(r0) < INFINITY ? r0 : 0.f, f, y0);
-          const float z = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, static_cast<float>(past))), pres);
-          x[c][e] = past ? z : x[c][e];
-        }
+          for (int e = 0; e < 8; ++e) {      // without branches: among 512 tokens of a wavefront some are in any history
+            const int past = k[e] & ((1 << LOGITS_COUNTS) - 1);
+            entries |= static_cast<unsigned>(k[e]);
+            const bool up = x[c][e] > 0.f;      // x / rep as logits_div(), otherwise x rep
+            float y;
+            if (plain()) {
+              const float f = up ? by_rep.r : rep, y0 = x[c][e] * f, r0 = __builtin_fmaf(-y0, rep, x[c][e]);
+              y = __builtin_fmaf(up && fabsf(r0) < INFINITY ? r0 : 0.f, f, y0);
+            } else {
+              y = up ? logits_div<false>(x[c][e], by_rep) : x[c][e] * rep;
+            }
+            const float z = __fsub_rn(__fsub_rn(y, __fmul_rn(freq, static_cast<float>(past))), pres);
+            x[c][e] = past ? z : x[c][e];
+          }
+        };
+        if (by_rep.plain) penalise(std::true_type{});
+        else penalise(std::false_type{});
         if (entries >> LOGITS_COUNTS) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
@@ -172,8 +195,13 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(EACH ==
       }
     }
     if (q.temperature) {
+      if (by_temp.plain) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[c][e] = logits_div(x[c][e], temp, temp_r);
+        for (int e = 0; e < 8; ++e) x[c][e] = logits_div<true>(x[c][e], by_temp);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[c][e] = logits_div<false>(x[c][e], by_temp);
+      }
     }
     if (mask) {
 #pragma unroll
