@@ -554,8 +554,9 @@ int ecospa_prefix_attn(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int 
  * dst (its k, v, strides and cap >= keep; B, h_kv and widths as src; must not overlap it): receives the kept rows; weights_out
  * (float[B, h_kv, dst->cap], NULL: not wanted) their weights, lens_out (int32[B]) the new lengths min(lens[b], keep), idx
  * (int32[B, h_kv, keep], NULL: not wanted) the kept rows' numbers, then -1.  Other rows of dst are left as they are.
- * Errors also: ERR_K (keep < 1, recent outside [0, keep], dst->cap < keep), ERR_SHAPE (lens_out is src->lens, which the launches
- * still read; an output is its own input).  Workspace (idx NULL only): B * h_kv * keep int32. */
+ * Errors also: ERR_K (keep < 1, recent outside [0, keep], dst->cap < keep), ERR_SHAPE (an output starts where an input or
+ * another output does, which the launches still read or write; overlaps further on are not looked for).  Workspace (idx NULL
+ * only): B * h_kv * keep int32. */
 int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src /*host*/, const float* weights, int keep, int recent,
                        const ecospa_cache* dst /*host*/, int* lens_out, float* weights_out, int* idx);
 

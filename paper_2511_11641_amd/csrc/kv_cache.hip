@@ -207,6 +207,15 @@ extern "C" int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src, cons
     idx = static_cast<int*>(ws.take(static_cast<size_t>(src->B) * src->h_kv * keep * sizeof(int)));
     if (!ws.ok()) return ECOSPA_ERR_WORKSPACE;
   }
+  // rows are gathered by many workgroups at once: what one of them writes, no other may still have to read
+  const void* const in[] = {src->k, src->v, src->lens, weights};
+  const void* const out[] = {d.k, d.v, lens_out, idx, weights_out};
+  for (int i = 0; i < 5; ++i) {
+    for (int j = 0; j < 4; ++j)
+      if (out[i] == in[j]) return ECOSPA_ERR_SHAPE;
+    for (int j = 0; j < i; ++j)
+      if (out[i] && out[i] == out[j]) return ECOSPA_ERR_SHAPE;
+  }
   a.k = static_cast<const bf16_t*>(src->k); a.v = static_cast<const bf16_t*>(src->v);
   a.k_out = static_cast<bf16_t*>(d.k); a.v_out = static_cast<bf16_t*>(d.v);
   a.weights = weights; a.weights_out = weights_out; a.lens = src->lens; a.lens_out = lens_out; a.idx = idx;
