@@ -32,6 +32,7 @@ class Server:
         assert stack.pos is None or max_pos <= stack.pos.w.shape[0], "positions beyond the learned table"
         bf, dev = torch.bfloat16, "cuda"
         self.P, self.longest = 0, 0               # tokens of the prefix; upper bound on the own lengths (known here, so that calls can be cut)
+        self.used = 0                             # positions that every request has behind it, prefix and evicted tokens among them
         self.lens = torch.zeros(Bsz, dtype=torch.int32, device=dev)
         self.pos = torch.zeros(Bsz, dtype=torch.int32, device=dev)         # position of a request's next token
         self.layers, self.spare = [], None
@@ -79,7 +80,8 @@ class Server:
     def set_prefix(self, ids: torch.Tensor):
         """The prefix that every request starts with (int64 [P]; P <= max_pos): runs it once and empties the requests' own caches."""
         st, ctx, P = self.st, self.ctx, ids.numel()
-        self.P, self.longest = P, 0
+        assert P <= self.max_pos, f"a prefix of {P} tokens, tables of {self.max_pos} positions"
+        self.P, self.longest, self.used = P, 0, P
         self.lens.zero_()
         self.pos.fill_(P)
         one, whole = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.full((1,), P, dtype=torch.int32, device="cuda")
@@ -105,6 +107,9 @@ class Server:
             res = self._ffn(ly["ffn"], y)
         self._caches()
 
+    def _room(self, L: int):
+        assert self.used + L <= self.max_pos, f"{L} tokens behind {self.used}, tables of {self.max_pos} positions"
+
     def _lse(self, n: int) -> torch.Tensor:
         if getattr(self, "_lse_buf", None) is None or self._lse_buf.numel() < n:
             self._lse_buf = torch.empty(n, dtype=torch.float32, device="cuda")
@@ -112,11 +117,15 @@ class Server:
 
     @torch.no_grad()
     def feed(self, ids: torch.Tensor) -> torch.Tensor:
-        """The next L tokens of every request (int64 [Bsz, L]) -> logits of the last ones, bf16 [Bsz, vocab] (a buffer of this object)."""
+        """The next L tokens of every request (int64 [Bsz, L]) -> logits of the last ones, bf16 [Bsz, vocab] (a buffer of this object).
+        Evictions make room in the caches, not in the tables: positions end with max_pos."""
         st, ctx = self.st, self.ctx
-        L = ids.shape[1]
+        n, L = ids.shape
+        assert n == self.B, f"tokens of {n} requests, built for {self.B}"
+        self._room(L)
         assert self.longest + L <= self.cap, "the caches are full: evict() first"
         T = self.B * L
+        self.used += L
         self.longest += L
         self.lens += L
         x, res = self._embed(ids.reshape(-1), self.pos, L)
@@ -157,6 +166,7 @@ class Server:
         ``Context.ecospa_logits_process``: repetition, frequency, presence, temperature, bias_ids, bias, mask, mask_row); the
         history of the penalties is the prompt and what came since.  Full caches are cut down to `keep` keys.  -> int32 [Bsz, steps]."""
         Bsz, L = prompts.shape
+        self._room(L + max(steps - 1, 0))         # the last token is not fed
         history = torch.zeros((Bsz, L + steps), dtype=torch.int32, device="cuda")
         history[:, :L] = prompts
         seen = torch.full((Bsz,), L, dtype=torch.int32, device="cuda")
