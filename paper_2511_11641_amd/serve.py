@@ -24,8 +24,9 @@ from .stack import DecoderStack
 
 class Server:
     """``Bsz`` requests on the compact weights of a :class:`.stack.DecoderStack` (its first estimate is done when it is built), with room
-    for ``cap`` own tokens each and positions up to ``max_pos``.  evictable: keep the attention weight of every own key (what
-    :meth:`evict` goes by)."""
+    for ``cap`` own tokens each and positions up to ``max_pos``.  Requests share no prefix until :meth:`set_prefix` gives them one.
+    evictable: keep the attention weight of every own key (what :meth:`evict` goes by).  The stack's weights stay as they are while this
+    object is in use: a new estimate needs a new one."""
 
     def __init__(self, stack: DecoderStack, Bsz: int, cap: int, max_pos: int, evictable: bool = True):
         self.st, self.ctx, self.B, self.cap, self.max_pos = stack, stack.ctx, Bsz, cap, max_pos
@@ -44,6 +45,7 @@ class Server:
             if evictable and self.spare is None:  # what an eviction writes into; the cache it leaves is the next layer's
                 self.spare = (*kv(Bsz), torch.zeros((Bsz, a.h_kv, cap), dtype=torch.float32, device=dev))
         self._buffers, self._descs = {}, {}
+        self._caches()                            # without a prefix until there is one
 
     def _buf(self, name: str, rows: int, width: int) -> torch.Tensor:
         key = (name, rows, width)
