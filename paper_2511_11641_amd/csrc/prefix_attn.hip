@@ -341,12 +341,16 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
   } else {
     p.own = own;
     plan_joint(a, p, true);
-    // Prompts: 64 rows a wavefront halve the reads of LDS, where narrow heads leave the registers and there are workgroups enough for two on every
-    // compute unit several times over (16 x 509 tokens on 8192, 4 query heads a key/value head: 653 -> 618 us; 8 x 256 on 2048 with its half as
-    // many workgroups: 43 -> 48).
-    if (own == ROWS_128 && !prefix_wide(p.dq, p.dv) && a.slots == 0 && static_cast<long long>(a.B) * a.h_kv * ceil_div(a.own_rows, 256) >= 1024) {
+    // Prompts: 64 rows a wavefront halve the reads of LDS, where narrow heads leave the registers.  A compute unit holds two such workgroups.  From two
+    // rounds of them on, at equal padding, against items of 128 rows: 0.93 to 0.95 of the time with 64 + 64 dims and 4096 prefix keys or more, 0.94 to
+    // 0.97 with 96 in all, 0.95 to 1.01 with 1000; but 1.06 with 500 + 250 keys; with 32 + 32 dims 1.06 with 1000, 0.98 to 1.01 with 4096, 0.98 with 8192.
+    // One more of the 128-row tiles padded is lost (300 rows, 2000 + 400 keys: 265 us against 180).  Under two rounds it depends on how full the last is (509
+    // tokens of 4 query heads on 8192 keys, 512 / 640 / 768 / 896 / 960 workgroups: 0.92 / 1.10 / 0.95 / 1.03 / 0.94): left with 128.
+    const long long tiles_256 = ceil_div(a.own_rows, 256), keys = static_cast<long long>(a.P) + a.own_max;
+    if (own == ROWS_128 && !prefix_wide(p.dq, p.dv) && a.slots == 0 && static_cast<long long>(a.B) * a.h_kv * tiles_256 >= 2 * 2 * 256 &&
+        a.o_row_tiles == 2 * tiles_256 && keys >= (p.dq + p.dv > 64 ? 1024 : 4096)) {
       p.own = ROWS_256;
-      a.o_row_tiles = static_cast<int>(ceil_div(a.own_rows, 256));
+      a.o_row_tiles = static_cast<int>(tiles_256);
       plan_joint(a, p, true);
     }
   }
