@@ -189,8 +189,9 @@ extern "C" int ecospa_cache_evict(ecospa_ctx* ctx, const ecospa_cache* src, cons
   if (!ctx || !src || !dst || !weights || !lens_out || !dst->k || !dst->v) return ECOSPA_ERR_NULL;
   int rc = ecospa_cache_check(src);
   if (rc != ECOSPA_OK) return rc;
-  ecospa_cache d = *dst;      // its lengths are an output, its prefix and bound play no part
+  ecospa_cache d = *dst;      // its lengths are an output, its query heads, prefix and bound play no part
   d.lens = lens_out;
+  d.h = src->h;
   d.P = 0;
   d.own_max = 0;
   d.scale = src->scale;

@@ -33,3 +33,8 @@ def test_outputs_that_are_inputs(lib, ctx, change, listed):  # noqa: F811
 
 def test_the_same_call_apart_is_not_refused(lib, ctx):  # noqa: F811
     assert call(lib, ctx, idx=None) == B.ERR_WORKSPACE   # no refusal of its arguments: the next one is for the memory that is missing
+
+
+@pytest.mark.parametrize("h", [0, 6, 4, 8])
+def test_the_query_heads_of_the_new_cache_play_no_part(lib, ctx, h):  # noqa: F811
+    assert call(lib, ctx, idx=None, h=h) == B.ERR_WORKSPACE
