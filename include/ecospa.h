@@ -493,7 +493,9 @@ int ecospa_xent(ecospa_ctx* ctx, int T, int V, int dtype, const void* logits, lo
 /* ------------------------------------------------------------------------------------------
  * Serving a compact model token by token.  The keys and values of the tokens that a request has behind it are kept in a cache of
  * compact heads (only the kept dims of a head are stored); a prefix that all requests of a batch share - a system prompt, a
- * document - is kept once for all of them.  bf16 storage, as the attention block; fp32 arithmetic; results repeat bit for bit.
+ * document - is kept once for all of them.  bf16 storage, as the attention block; fp32 arithmetic, but the probabilities enter their
+ * product with the values rounded to bf16, as the attention block's do (sums, lse and weights come from the unrounded ones); results
+ * repeat bit for bit.
  *
  * ecospa_cache: B requests, each with `lens[b]` keys of its own (device int32, read when the kernels run; a length outside
  * [0, own_max] counts as the nearer bound), the tokens of the present call among them: the L new tokens of a call are the last L
@@ -501,7 +503,9 @@ int ecospa_xent(ecospa_ctx* ctx, int T, int V, int dtype, const void* logits, lo
  * + j*v_st (kp_vo elements); prefix row j at pk + g*pk_sh + j*pk_st and pv + g*pv_sh + j*pv_st - e.g. the K and V columns of the
  * saved qkv rows of an ecospa_coupled_fwd over the prefix, or a cache of one request that ecospa_cache_append filled.  Strides in
  * elements, multiples of 8, at most 2^25 - 1 between rows; pointers 16-byte aligned.  kp_qk, kp_vo: multiples of 16 up to 128.
- * own_max: no request holds more than this many own keys (0: none has any); it only bounds the work, cap bounds the memory.
+ * own_max: no request holds more than this many own keys (0: none has any).  It bounds the work, cap bounds the memory, and calls are
+ * cut by it: own keys of more than 96 MB by this bound are read past the last-level cache, so a bound far above the real lengths
+ * costs time.  ecospa_cache_append goes by the lengths as they are.
  * Rows at and beyond lens[b] are never read.
  * Common errors, before any launch: ERR_NULL; ERR_DTYPE (dtype other than ECOSPA_BF16); ERR_SHAPE (B, h_kv, cap, L < 1; h_kv does
  * not divide h; widths; own_max outside [0, cap]; P < 0; scale not a positive number; row strides; B * h_kv > 65535, B * L * h >

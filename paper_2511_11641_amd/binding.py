@@ -266,7 +266,8 @@ class KvCache:
 
     k: [B, h_kv, cap, kp_qk], v: [B, h_kv, cap, kp_vo] (bf16, last dim dense, other strides free); lens: int32 [B], own keys of every
     request; h query heads; scale: the softmax scale; pk: [h_kv, P, kp_qk], pv: [h_kv, P, kp_vo] or None.  own_max (default: cap): no
-    request holds more keys than this, a smaller bound saves work; it may be set between calls.  The object keeps the tensors alive;
+    request holds more keys than this; calls are cut by it, so a bound near the real lengths saves work and keeps small caches in the
+    last-level cache; it may be set between calls.  The object keeps the tensors alive;
     their contents, lens included, are read when the kernels run."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, lens: torch.Tensor, h: int, scale: float, pk: Optional[torch.Tensor] = None,

@@ -7,8 +7,8 @@
 // one range is the row).  Nothing is added in an order that varies: results repeat bit for bit.
 //
 // The penalties, a temperature and the exponential are about 50 vector instructions a logit, beside 4 to 8 bytes of memory: 256 x 131072 fp32 with
-// histories of 8192 take 64.4 us, 4.2 TB/s, the vector unit 75 % busy; with histories
-// of 100 55.6 us, 4.8 TB/s.  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
+// histories of 8192, which every one of 16 ranges looks through, take 64.8 us, 4.1 TB/s, the vector unit 77 % busy; with histories of 100 55.2 us,
+// 4.9 TB/s (calls one behind the other, the join among them).  Few rows are bound by latencies: 1 x 32000 bf16 5.9 us.
 #include "common.h"
 
 #include <type_traits>
@@ -288,13 +288,13 @@ __global__ __launch_bounds__(256) void logits_join_kernel(const LogitsArgs a) {
   if (lane == 0) logits_finish(a, b, m, s, at == 0xffffffffu ? -1 : static_cast<int>(at));
 }
 
-// Threads, logits a thread and tokens of a workgroup.  A vocabulary that one workgroup holds needs no join (256 x 9000 bf16, histories of 2000:
-// one range of 1024 threads 7.4 us, two of 512 and the join 9.9).  Else 16 logits a thread in workgroups of 512, of which a compute unit holds four
-// (256 x 131072 fp32, histories of 8192: 76 us; 32 a thread 80, 8 a thread 95, before the stores passed the caches by; since, 64.4, and workgroups of
-// 1024 65.8, with histories of 100 55.6 and 61.4), and 8 in workgroups of 256 while all of them are resident at once and shorter passes end sooner (1 x
-// 32000: 5.8 us against 7.0; 64 x 32000 8.6 against 8.7).  Rows of up to 32768 bf16 logits for most compute units, but not more than one each: a
-// workgroup a row, 32 logits a thread, which saves the join and reads the history once (32000, histories of 1000, 160 / 192 / 224 / 256 rows: 11.1 /
-// 11.5 / 11.8 / 12.4 us against 11.9 / 12.2 / 14.1 / 14.6; but 128 rows 11.9 against 11.2, 320 rows 21.2 against 16.5; fp32 256 rows 19.9 against 16.8).
+// Threads, logits a thread and tokens of a workgroup. A vocabulary that one workgroup holds needs no join (256 x 9000 bf16, histories of 2000:
+// one range of 1024 threads 7.4 us, two of 512 and the join 9.9).  Else 16 logits a thread in workgroups of 512, of which a compute unit holds four (256 x
+// 131072 fp32, histories of 8192 / 100: workgroups of 512 64.4 / 55.6 us, of 1024 65.8 / 61.4; 32 logits a thread were 5 %, 8 were 25 % slower), and 8 in
+// workgroups of 256 while all of them are resident at once and shorter passes end sooner (1 x 32000: 5.8 us against 7.0; 64 x 32000 8.6 against 8.7).
+// Rows of up to 32768 bf16 logits for most compute units, but not more than one each: a workgroup a row, 32 logits a thread, which saves the join and
+// reads the history once.  Against 16 a thread, seven vocabularies from 16500 to 32768, histories of 1000: 160 rows 0.92 to 1.04 of the time, 192 0.83 to
+// 0.96, 224 and 256 0.82 to 0.89 (histories of 8000 0.71 to 0.79); but 272 rows 1.25 to 1.36, 128 rows 0.98 to 1.13.  In fp32 256 rows 19.9 us against 16.8.
 struct LogitsPlan { int threads, each, range, ranges; };
 static LogitsPlan logits_plan(int B, int V, bool bf) {
   LogitsPlan p;

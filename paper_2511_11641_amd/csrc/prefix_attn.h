@@ -16,8 +16,8 @@
 //
 // What bounds it (heads of 64 + 64 dims): one token a request on own caches alone, memory - 64 x 8 heads x 2048 keys, 268 MB, 44.7 us, 6.0 TB/s of the
 // 6.3 that a plain read reaches.  Rows of many requests on a prefix, the vector unit: an exponential takes a SIMD about as long as the matrix products
-// of its score, and maximum, scaling, sum and conversion as long again - 256 rows x 8 heads on 32768 keys 41 us, 417 TFLOP/s with its join; 16 x 509 tokens on 8192 keys 612 us, 950 TFLOP/s, at the clock that
-// power allows (1.9 GHz).  Both at once, 64 requests on 32768 + 2048 keys: 71 us.  A single short request, latency: 61 + 33 keys 4.5 us.
+// of its score, and maximum, scaling, sum and conversion as long again - 256 rows x 8 heads on 32768 keys 41 us, 417 TFLOP/s with its join; 16 x 509 tokens on 8192 keys and their own 620 us, 909
+// TFLOP/s by the pairs that see each other, at the clock that power allows (1.9 GHz).  Both at once, 64 requests on 32768 + 2048 keys with weights: 65 us.  A single short request, latency: 61 + 33 keys 4.5 us.
 //
 // Only a row that sees no key has a sum of exponentials of zero; it is told by that.  A row that meets a score that is not a number, or +inf, has a sum,
 // an output, a log-sum-exp and weights that are not numbers, in whatever piece the key lies (its maximum may say -inf: maxima pass over NaN).

@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(const PrefixArgs a, in
 // Weights: w_out[j] = w_in[j] + sum over the rows of the request that see own key j of exp(s_j - lse).  Keys stay in registers while the rows pass by from
 // the first that sees a key, 32 at a time, the next ones on their way; S^T = K Q^T, so that the sum over rows is a sum over lanes, taken once at the end.
 // MANY rows: 64 keys a workgroup, its wavefronts take the rows in turn.  Otherwise 32 keys a wavefront, and no key is read twice.  Bound by the latency
-// of the rows' reads, then by the exponentials: 16 x 509 tokens of 32 heads on their own 509 keys 36 us, the attention itself 611.
+// of the rows' reads, then by the exponentials: 16 x 509 tokens of 32 heads on their own 509 keys 36 us, the attention itself 620.
 // ---------------------------------------------------------------------------------------------
 template <int DQ, bool MANY>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_weights_kernel(const PrefixArgs a, const float* lse, const float* w_in,
@@ -218,11 +218,10 @@ struct PrefixPlan {
 // What the items of a call cost, in ns, for the choice between ways to cut it.  Constants as measured: an item's start and end 3 us, a step's least time (a
 // latency of memory and what a compute unit can take in, or a tile of a wavefront that has a SIMD for itself: 1.4 us for 32 rows of 64 + 64 dims), 5.5
 // bytes/ps of memory over all workgroups (`share` of them read the same keys), and a row and key of a tile on a compute unit (heads of 64 + 64 dims 0.08
-// ns; the unused rows of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them such items.  Chunks of the prefix forced to
-// other counts (8 to 48, 1 and 2 of own keys): the choice is within 1 % of the best for 64 requests on 32768 tokens (15 chosen, 12 best; with weights 81 us
-// against 77), for 12 x 5 on 8191 and 8 on 2000 the best, for 32 on 4096 21.0 us against 19.4 (6 chosen, 3 best).  Over 200 random shapes, joint items or
-// items apart forced, the choice lost 1.4 % in the mean against the better one, 39 % at most (16.4 us against 11.8); the join's 4 us and the 7 ns a dim of
-// a step, set after that, took 0.3 % off 600 shapes (0.67 to 1.075 of the time each).
+// ns; the unused rows of a tile cost as much).  keys: of the item; active: workgroups at work, `alike` of them such items.  How good the choice is: with
+// the chunks of the prefix forced to other counts (8 to 48, 1 and 2 of own keys) it is the best for 12 x 5 tokens on 8191 and for 8 on 2000, within 1 % for
+// 64 on 32768, but 5 % off the best with weights (15 chosen, 12 best), and 8 % off for 32 on 4096 (6 chosen, 3 best): the model has no term for a last
+// round of workgroups that is partly filled.  Joint items or items apart forced over 200 random shapes: 1.4 % lost in the mean, 39 % at most.
 struct ItemCost { double step, item; };
 static ItemCost item_cost(const PrefixArgs& a, const PrefixPlan& p, int kind, double steps, double keys, double active, double alike, double share) {
   const double per_cu = std::ceil(alike / 256), step_keys = keys_of(kind) * tiles_at_once(kind);
@@ -354,7 +353,8 @@ static bool prefix_plan(PrefixArgs& a, PrefixPlan& p, bool weights) {
       plan_joint(a, p, true);
     }
   }
-  // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call: their loads pass the caches by.  Own
+  // Keys that no other item reads, and more of them than the last cache (256 MB) keeps until a next call, by own_max where lengths are on the device
+  // (short caches under a far larger own_max give up what the cache would have kept: the header says so): their loads pass the caches by.  Own
   // caches of 134 MB 27.5 -> 23.9 us, 100 MB 21.6 -> 19.9, 268 MB 51.4 -> 44.5; a prefix of 268 MB 55.0 -> 48.0.  With 67 MB it depends on what
   // passes between two calls: 17.2 -> 15.2 where the cache had lost them, 14.0 -> 14.9 where it had not.
   const auto once = [&](double heads, double keys, int row_tiles) { return row_tiles == 1 && heads * keys * (a.kq + a.kv) * 2 > 96e6; };

@@ -166,7 +166,8 @@ class Server:
     def generate(self, prompts: torch.Tensor, steps: int, *, keep: Optional[int] = None, recent: int = 0, **control):
         """`steps` tokens behind the prompts (int64 [Bsz, L]), the best one each time after `control` (the keyword arguments of
         ``Context.ecospa_logits_process``: repetition, frequency, presence, temperature, bias_ids, bias, mask, mask_row); the
-        history of the penalties is the prompt and what came since.  Full caches are cut down to `keep` keys.  -> int32 [Bsz, steps]."""
+        history of the penalties is the prompt and what came since.  Full caches are cut down to `keep` keys.  -> int32 [Bsz, steps]; -1
+        where no token was left to pick (everything masked, or not a number), and token 0 is fed in its place."""
         Bsz, L = prompts.shape
         self._room(L + max(steps - 1, 0))         # the last token is not fed
         history = torch.zeros((Bsz, L + steps), dtype=torch.int32, device="cuda")
