@@ -541,7 +541,8 @@ int ecospa_cache_append(ecospa_ctx* ctx, const ecospa_cache* cache /*host*/, int
  * prefix keys and the own keys j < lens[b] - L + 1 + t.  Prefix keys are read once for all requests.  q [B*L, h*kp_qk] (ld_q),
  * o [B*L, h*kp_vo] (ld_o); query head i uses key/value head i / (h / h_kv).  lse (float[B, h, L], NULL: not wanted) receives
  * log sum exp of the scaled scores.  A query that sees no key has o = 0 and lse = -inf.
- * A query that is not a number, or sees a key with a score of NaN or +inf, has NaN for o, lse and the weights of the keys it sees.
+ * A query that is not a number, or sees a key with a score of NaN or +inf, has NaN for o, lse and the weights of the keys it sees
+ * (a key with an infinite element may count as such whatever its sign: padded dims multiply it by zero).
  * weights_out (float[B, h_kv, cap], NULL: not wanted): for every own key j < lens[b], weights_in (same layout, may be weights_out
  * itself; NULL: zeros) plus the probabilities that the queries of its group gave it: the accumulated attention weight that
  * ecospa_cache_evict goes by.  Entries beyond lens[b] are left as they are.
