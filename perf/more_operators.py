@@ -198,18 +198,18 @@ def _own(st):
     if case["kind"] == "linear":
         act = {"none": None, "gelu": B.ACT_GELU_ERF, "swiglu": B.ACT_SWIGLU}[case["act"]]
         x, s = ctx.ecospa_quant_rows(st["x"])
-        return {"y": ctx.ecospa_contract_i8(x, s, st["w"], st["sw"], bias=st["bias"], act=act, out=st["y"])}
+        return {"y": ctx.ecospa_contract_quant(x, s, st["w"], st["sw"], bias=st["bias"], act=act, out=st["y"])}
     if case["kind"] == "sample":
         ctx.ecospa_sample(st["logits"], st["u"], temperature=st["temp"], top_k=st["top_k"], top_p=st["top_p"], min_p=st["min_p"], token=st["token"], prob=st["prob"])
         return {"token": st["token"], "prob": st["prob"]}
     if "cache" not in st:                                  # a program keeps its cache object beside the cache
-        st["cache"] = B.KvCache8(st["k"], st["v"], st["k_scale"], st["v_scale"], st["lens"], case["h"], _scale(case), case["block"],
+        st["cache"] = B.QuantCache(st["k"], st["v"], st["k_scale"], st["v_scale"], st["lens"], case["h"], _scale(case), case["block"],
                                  own_max=case.get("own", case["cap"]))
     if case["kind"] == "append":
         rope = (st["cos"], st["sin"]) if case["rope"] else None
-        ctx.ecospa_cache8_append(st["cache"], st["qkv"], st["pos"], rope=rope, q=st["q"] if rope else None)
+        ctx.ecospa_quant_cache_append(st["cache"], st["qkv"], st["pos"], rope=rope, q=st["q"] if rope else None)
         return _cache_out(st)
-    ctx.ecospa_cache8_attn(st["cache"], st["q"], st["o"], lse=st["lse"], o_in=st.get("o_in"), lse_in=st.get("lse_in"))
+    ctx.ecospa_quant_cache_attn(st["cache"], st["q"], st["o"], lse=st["lse"], o_in=st.get("o_in"), lse_in=st.get("lse_in"))
     return {"o": st["o"], "lse": st["lse"]}
 
 
