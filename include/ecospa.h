@@ -36,7 +36,7 @@ enum { ECOSPA_OK = 0, ECOSPA_ERR_NULL = 1, ECOSPA_ERR_SHAPE = 2, ECOSPA_ERR_DTYP
 enum { ECOSPA_F32 = 0, ECOSPA_BF16 = 1 };
 enum { ECOSPA_PAIR_QK = 0, ECOSPA_PAIR_VO = 1, ECOSPA_PAIR_FFN = 2, ECOSPA_PAIR_FFN_GATED = 3 };
 enum { ECOSPA_BLOCK_ATTN = 0, ECOSPA_BLOCK_FFN = 1 };
-enum { ECOSPA_ACT_GELU_ERF = 0, ECOSPA_ACT_GELU_TANH = 1, ECOSPA_ACT_SWIGLU = 2 };
+enum { ECOSPA_ACT_NONE = -1 /* ecospa_contract_quant only */, ECOSPA_ACT_GELU_ERF = 0, ECOSPA_ACT_GELU_TANH = 1, ECOSPA_ACT_SWIGLU = 2 };
 
 typedef struct ecospa_ctx ecospa_ctx; /* host object */
 
@@ -600,6 +600,26 @@ typedef struct {
 } ecospa_logits;
 size_t ecospa_logits_workspace_bytes(int B, int V);
 int ecospa_logits_process(ecospa_ctx* ctx, const ecospa_logits* args /*host*/);
+
+/* ------------------------------------------------------------------------------------------
+ * Products in 8-bit integers.  A compact weight matrix is brought to 8 bits once, with a scale for each of its rows (output channels);
+ * activations are brought to 8 bits row by row (token by token) in front of every product.  A decoding step then reads half the weights' bytes, and the
+ * matrix units do twice the products in a cycle.
+ *
+ * ecospa_quant_rows: scale[r] = max_c |x[r, c]| / 127 and q[r, c] = x[r, c] / scale[r] rounded to the nearest whole number (half to even), both quotients
+ * those of an fp32 division, and no larger than 127 in size (a subnormal scale can be that coarse); where the scale is 0 the codes are.  A row that holds an infinity or NaN has scale NaN and zeros.  x: [rows, cols] of
+ * dtype ECOSPA_F32 or ECOSPA_BF16; q: int8 [rows, cols], must not overlap x.  cols a multiple of 8; x, q 16-byte aligned, ld a multiple of 8, ld_q of 16.
+ * Errors: ERR_NULL, ERR_DTYPE, ERR_SHAPE (rows < 1, cols < 8, cols % 8, a leading dimension below cols), ERR_ALIGN. */
+int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype, const void* x, long long ld, void* q, long long ld_q, float* scale);
+
+/* C[m, n] = act( sa[m] * sb[n] * sum_k A[m, k] B[n, k] + bias[n] ), A int8 [M, K], B int8 [N, K], sums in 32-bit integers (exact), scales and what follows in
+ * fp32, C bf16, rounded once.  bias: bf16 [N] or NULL.  act: ECOSPA_ACT_NONE, a GELU, or ECOSPA_ACT_SWIGLU, where columns come in (gate, up) pairs as in a block's
+ * w_1 and C is [M, N / 2], silu(gate) * up.  K a multiple of 16, N of 8 (SWIGLU: 16); A, B, C, bias and sb 16-byte aligned, lda and ldb multiples of 16,
+ * ldc of 8.  Needs no workspace.
+ * Errors: ERR_NULL; ERR_DTYPE (act); ERR_SHAPE (M < 1, N < 8, K outside [16, 131056], beyond which a sum could overflow; a leading dimension below its row, lda or
+ * ldb of 2^24 and more, ldc of 2^23 and more); ERR_ALIGN. */
+int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, long long lda, const float* sa, const void* B, long long ldb,
+                       const float* sb, const void* bias, int act, void* C, long long ldc);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ F32, BF16 = 0, 1
 PAIR_QK, PAIR_VO, PAIR_FFN, PAIR_FFN_GATED = range(4)
 BLOCK_ATTN, BLOCK_FFN = 0, 1
 ACT_GELU_ERF, ACT_GELU_TANH, ACT_SWIGLU = range(3)
+ACT_NONE = -1
 
 EXPORTS = (
     "ecospa_create", "ecospa_destroy", "ecospa_set_workspace", "ecospa_status_string", "ecospa_last_error",
@@ -34,6 +35,7 @@ EXPORTS = (
     "ecospa_norm_fwd", "ecospa_norm_bwd", "ecospa_norm_bwd_workspace_bytes", "ecospa_embed_fwd", "ecospa_embed_bwd", "ecospa_xent",
     "ecospa_cache_append", "ecospa_prefix_attn", "ecospa_prefix_attn_workspace_bytes", "ecospa_cache_evict",
     "ecospa_logits_process", "ecospa_logits_workspace_bytes",
+    "ecospa_quant_rows", "ecospa_contract_quant",
 )
 NORM_RMS, NORM_LAYER = 0, 1
 
@@ -228,6 +230,10 @@ def load() -> C.CDLL:
     lib.ecospa_logits_process.restype = ci
     lib.ecospa_logits_workspace_bytes.argtypes = [ci, ci]
     lib.ecospa_logits_workspace_bytes.restype = sz
+    lib.ecospa_quant_rows.argtypes = [vp, ci, ci, ci, vp, ll, vp, ll, vp]
+    lib.ecospa_quant_rows.restype = ci
+    lib.ecospa_contract_quant.argtypes = [vp, ci, ci, ci, vp, ll, vp, vp, ll, vp, vp, ci, vp, ll]
+    lib.ecospa_contract_quant.restype = ci
     _lib = lib
     return lib
 
@@ -772,6 +778,35 @@ class Context:
                    ids_ptr, bias_ptr, mask_ptr, _dense(mask_row, i32, Bsz), ld_mask, n_masks, _dense(pick, i32, Bsz), _dense(lse, f32, Bsz))
         self._check(self.lib.ecospa_logits_process(self.h, C.byref(a)), "ecospa_logits_process")
         return pick, lse
+
+    # ---- products in 8-bit integers --------------------------------------------------------------
+    def ecospa_quant_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+        """(q int8 [rows, cols], scale float32 [rows]) with x[r] ~ scale[r] * q[r]; x: [rows, cols] float32 or bf16, row stride free."""
+        (rows, cols), (ld, unit) = x.shape, x.stride()
+        q = torch.empty((rows, round_up(cols, 16)), dtype=torch.int8, device=x.device)[:, :cols] if q is None else q
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device) if scale is None else scale
+        if unit != 1 or q.dtype != torch.int8 or q.shape != x.shape or q.stride(1) != 1:
+            raise ValueError(f"expected rows of {cols} dense elements, got strides {x.stride()}, {q.dtype} {tuple(q.shape)} {q.stride()}")
+        self._check(self.lib.ecospa_quant_rows(self.h, rows, cols, dtype_code(x.dtype), x.data_ptr(), ld, q.data_ptr(), q.stride(0),
+                                               _dense(scale, torch.float32, rows)), "ecospa_quant_rows")
+        return q, scale
+
+    def ecospa_contract_quant(self, A: torch.Tensor, sa: torch.Tensor, Bm: torch.Tensor, sb: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                           act: Optional[int] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """act(sa[m] sb[n] sum_k A[m, k] B[n, k] + bias[n]) in bf16 [M, N] (SwiGLU: [M, N / 2]); A [M, K], Bm [N, K] int8 as
+        :meth:`ecospa_quant_rows` leaves them."""
+        (M, K), (lda, ua), (N, Kb), (ldb, ub) = A.shape, A.stride(), Bm.shape, Bm.stride()
+        act = ACT_NONE if act is None else act
+        width = N // 2 if act == ACT_SWIGLU else N
+        out = torch.empty((M, width), dtype=torch.bfloat16, device=A.device) if out is None else out
+        if A.dtype != torch.int8 or Bm.dtype != torch.int8 or Kb != K or ua != 1 or ub != 1:
+            raise ValueError(f"expected int8 rows of equal length, got {A.dtype} {tuple(A.shape)} and {Bm.dtype} {tuple(Bm.shape)}")
+        if out.dtype != torch.bfloat16 or out.shape != (M, width) or out.stride(1) != 1:
+            raise ValueError(f"expected a bf16 output [{M}, {width}], got {out.dtype} {tuple(out.shape)}")
+        self._check(self.lib.ecospa_contract_quant(self.h, M, N, K, A.data_ptr(), lda, _dense(sa, torch.float32, M), Bm.data_ptr(), ldb,
+                                                _dense(sb, torch.float32, N), _dense(bias, torch.bfloat16, N), act, out.data_ptr(), out.stride(0)),
+                    "ecospa_contract_quant")
+        return out
 
     # ---- parameter update ----------------------------------------------------------------------
     @staticmethod

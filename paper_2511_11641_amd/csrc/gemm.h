@@ -58,6 +58,17 @@ struct GemmDesc {
 
 // Launch on ctx->stream.  bf16 and fp32 both run on MFMA tiles.
 int ecospa_gemm(ecospa_ctx* ctx, const GemmDesc& d);
+// x W^T of 8-bit integers, 32-bit sums (contract_i8.hip).  The matrix unit takes 16 of them where it takes 8 bf16, in the same registers, and
+// everything in front of it moves bytes: the kernels are those of bf16 with another product and epilogue, and K, lda and ldb of the
+// descriptor count pairs of integers.
+int ecospa_gemm_i8(ecospa_ctx* ctx, const GemmDesc& d);
+#define GEMM_EPIS_I8 ((1 << EPI_STORE) | (1 << EPI_ACT) | (1 << EPI_SWIGLU))
+// Scales of the rows of A and of B, in fields that these kinds of epilogue leave free: a sum enters the epilogue as fma(sum * sa[m], sb[n], bias[n]).
+__host__ __device__ static inline const float* gemm_i8_sa(const GemmEpi& e) { return static_cast<const float*>(e.h); }
+__host__ __device__ static inline const float* gemm_i8_sb(const GemmEpi& e) { return e.rope_cos; }
+hipError_t gemm_share_launch_i8(ecospa_ctx* ctx, const GemmDesc& d, int shape);
+hipError_t gemm_flow_launch_i8(ecospa_ctx* ctx, const GemmDesc& d);
+hipError_t gemm_ring_launch_i8(ecospa_ctx* ctx, const GemmDesc& d, int shape);
 // Two contractions that do not depend on each other: w a weight gradient (dY^T X, bf16 or fp32; its reduction deferred where K is split), x
 // over the same tokens.  One launch where that is built for the two and pays, otherwise w, then x (x_first: the other way round).
 int ecospa_gemm_pair(ecospa_ctx* ctx, const GemmDesc& w, const GemmDesc& x, int x_first = 0);

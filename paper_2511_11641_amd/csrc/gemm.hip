@@ -567,6 +567,25 @@ int ecospa_gemm(ecospa_ctx* ctx, const GemmDesc& d) {
   return ECOSPA_OK;
 }
 
+// 8-bit integers: never split along K (a sum of few tokens is shared out inside the workgroups), and the choice is that of bf16 operands of as many bytes.
+int ecospa_gemm_i8(ecospa_ctx* ctx, const GemmDesc& d) {
+  if (d.trans_a || d.trans_b || d.splits > 1 || d.colsum || !((GEMM_EPIS_I8 >> d.epi.kind) & 1)) return ECOSPA_ERR_DTYPE;
+  if (!gemm_i8_sa(d.epi) || !gemm_i8_sb(d.epi)) return ECOSPA_ERR_NULL;
+  if (!aligned16(gemm_i8_sb(d.epi))) return ECOSPA_ERR_ALIGN;
+  if (ring_wide(d)) return ECOSPA_ERR_SHAPE;
+  GemmDesc as_bf16 = d;
+  as_bf16.dtype = ECOSPA_BF16;
+  const int bad = gemm_check(as_bf16);
+  if (bad) return bad;
+  const int shape = ecospa_gemm_route(as_bf16);
+  const bool prof = prof_begin(ctx);
+  const hipError_t le = shape >= GEMM_ROUTE_SHARE ? gemm_share_launch_i8(ctx, d, shape - GEMM_ROUTE_SHARE) : shape == GEMM_ROUTE_FLOW ? gemm_flow_launch_i8(ctx, d) : gemm_ring_launch_i8(ctx, d, shape);
+  if (le != hipSuccess) return hip_fail(ctx, le, "gemm_i8 launch");
+  if (prof) prof_end(ctx, 4.0 * d.M * d.N * d.K);
+  ECOSPA_CHECK_LAUNCH(ctx, "gemm_i8");
+  return ECOSPA_OK;
+}
+
 // Byte ranges that a descriptor reads and writes.
 struct GemmRange {
   uintptr_t lo, hi;

@@ -153,7 +153,8 @@ struct FlowDeal {
   static constexpr int groups_upto(int b) { return 2 * b <= 2 ? 0 : b >= NB ? GROUPS : (first(2 * b, 0) + FlowEpi<KIND>::PIECES - 1) / FlowEpi<KIND>::PIECES; }
 };
 
-template <int BM, int BN, int NS, bool TA, bool TB, int KIND, int NB>
+// I8: operands of 8-bit integers (ecospa_gemm_i8).
+template <int BM, int BN, int NS, bool TA, bool TB, int KIND, int NB, bool I8 = false>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
   constexpr int WTM = BM / 2, WTN = BN / 2, FM = WTM / 16, FN = WTN / 16, S = RING_BK / 32, NM = FM * FN, NR = FM + FN, JP = FN / 2;
@@ -264,6 +265,7 @@ void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
   EpiSide side[epi_has_side(KIND) ? GROUPS : 1];      // (a few of them live at a time)
   float bias[Epi::BIAS ? JP : 1][8];
   uint4 braw[JP];
+  float sa[I8 ? FM : 1], sb[I8 ? JP : 1][8];
   int pm0 = 0, pn0 = 0;
   int col[JP], rope_off[KIND == EPI_ROPE ? JP : 1];
   bool rope_on[KIND == EPI_ROPE ? JP : 1];
@@ -292,12 +294,25 @@ void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
         rope_on[jp] = n < d.epi.rope_cols;
         rope_off[jp] = rope_on[jp] ? (row * d.epi.rope_L) * (d.epi.rope_kp / 2) + (n % d.epi.rope_kp) / 2 : 0;
       }
+      if constexpr (I8) ring_i8_scales(gemm_i8_sb(d.epi) + pn0 + col[jp], sb[jp]);
+    }
+    if constexpr (I8) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) sa[i] = gemm_i8_sa(d.epi)[pm0 + row_of(i)];
     }
   };
   auto epi_bias = [&]() __attribute__((always_inline)) {
     if constexpr (Epi::BIAS) {
 #pragma unroll
       for (int jp = 0; jp < JP; ++jp) unpack8(braw[jp], bias[jp]);
+    }
+    if constexpr (I8) {      // in registers before the first piece uses them: one wait
+#pragma unroll
+      for (int jp = 0; jp < JP; ++jp)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(sb[jp][q]));
+#pragma unroll
+      for (int i = 0; i < FM; ++i) asm volatile("" : "+v"(sa[i]));
     }
   };
   auto request = [&](auto g_) __attribute__((always_inline)) {   // side inputs of group g
@@ -322,11 +337,14 @@ void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
       const EpiSide& sd = side[epi_has_side(KIND) ? gi : 0];
       if constexpr (p < Epi::P0) {
         const auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(from[i][2 * jp][p]), __float_as_uint(from[i][2 * jp + 1][p]), false, false);
-        ep.x[p] = __uint_as_float(w[0]);
-        ep.x[4 + p] = __uint_as_float(w[1]);
+        ep.x[p] = I8 ? ring_i8_row(w[0], sa[I8 ? i : 0]) : __uint_as_float(w[0]);
+        ep.x[4 + p] = I8 ? ring_i8_row(w[1], sa[I8 ? i : 0]) : __uint_as_float(w[1]);
       } else if constexpr (p < Epi::P1) {
 #pragma unroll
-        for (int q = 4 * (p - Epi::P0); q < 4 * (p - Epi::P0) + 4; ++q) ep.x[q] += bias[Epi::BIAS ? jp : 0][q];
+        for (int q = 4 * (p - Epi::P0); q < 4 * (p - Epi::P0) + 4; ++q) {
+          if constexpr (I8) ep.x[q] = __builtin_fmaf(ep.x[q], sb[jp][q], bias[Epi::BIAS ? jp : 0][q]);
+          else ep.x[q] += bias[Epi::BIAS ? jp : 0][q];
+        }
       } else if constexpr (p < Epi::PIECES - 1) {
         constexpr int st = (p - Epi::P1) / 2, q0 = 4 * ((p - Epi::P1) % 2);
 #pragma unroll
@@ -389,7 +407,10 @@ void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
       ring_for<0, NM>([&](auto m_) __attribute__((always_inline)) {
         constexpr int m = decltype(m_)::value, i = m / FN, j = m % FN;
         const bf16x8_t b = ring_val<TB>(fb[cur][j]), a = ring_val<TA>(fa[cur][i]);
-        if constexpr (ZERO && s == 0) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b), "v"(a));
+        if constexpr (I8) {
+          if constexpr (ZERO && s == 0) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b), "v"(a));
+          else ring_mfma_i8<true>(acc[i][j], b, a);
+        } else if constexpr (ZERO && s == 0) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc[i][j]) : "v"(b), "v"(a));
         else ring_mfma(acc[i][j], b, a);
         __builtin_amdgcn_sched_barrier(0);
         constexpr int R0 = m < RSLOTS ? m * NR / RSLOTS : NR, R1 = m < RSLOTS ? (m + 1) * NR / RSLOTS : NR;
@@ -475,13 +496,13 @@ void gemm_bf16_flow_kernel(const GemmDesc d, int tiles_n, int tiles) {
 
 // ---------------------------------------------------------------------------------------------
 // launch of a descriptor that gemm_flow_takes()
-template <bool TA, bool TB, int KIND>
+template <bool TA, bool TB, int KIND, bool I8 = false>
 static hipError_t flow_launch(ecospa_ctx* ctx, const GemmDesc& d) {
   const int tm = (d.M + FLOW_BM - 1) / FLOW_BM, tn = (d.N + FLOW_BN - 1) / FLOW_BN;
   constexpr int lds_bytes = FLOW_NS * (FLOW_BM + FLOW_BN) * RING_BK * static_cast<int>(sizeof(bf16_t));
   static_assert(lds_bytes > 64 * 1024 && lds_bytes <= 160 * 1024, "LDS of a compute unit");
   static_assert(FLOW_MIN_SLABS >= FLOW_NB + FLOW_NS, "the loads turn to the next tile behind the epilogue");
-  auto kern = gemm_bf16_flow_kernel<FLOW_BM, FLOW_BN, FLOW_NS, TA, TB, KIND, FLOW_NB>;
+  auto kern = gemm_bf16_flow_kernel<FLOW_BM, FLOW_BN, FLOW_NS, TA, TB, KIND, FLOW_NB, I8>;
   static LdsAttrOnce attr_once;
   const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), lds_bytes);
   if (e != hipSuccess) return e;

@@ -40,6 +40,7 @@ typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
 typedef unsigned int ring_u4 __attribute__((ext_vector_type(4)));
 typedef unsigned int ring_u2 __attribute__((ext_vector_type(2)));
 typedef float ring_f4 __attribute__((ext_vector_type(4)));
+typedef int ring_i4 __attribute__((ext_vector_type(4)));
 
 #define RING_BK 64
 
@@ -163,6 +164,20 @@ template <bool KS> __device__ __forceinline__ bf16x8_t ring_val(const RingFrag& 
 __device__ __forceinline__ void ring_mfma(ring_f4& c, const bf16x8_t& a, const bf16x8_t& b) {
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
 }
+// 64 products of 8-bit integers: the accumulators hold 32-bit integers.  FULL: the accumulators fill the AGPRs.  Elsewhere the compiler keeps one
+// of them in VGPRs where control flow joins; it knows the waits that such moves need beside its own instruction only.
+template <bool FULL>
+__device__ __forceinline__ void ring_mfma_i8(ring_f4& c, const bf16x8_t& a, const bf16x8_t& b) {
+  if constexpr (FULL) asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else c = __builtin_bit_cast(ring_f4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(ring_i4, a), __builtin_bit_cast(ring_i4, b), __builtin_bit_cast(ring_i4, c), 0, 0, 0));
+}
+// An integer sum in front of its epilogue, rounded to fp32 and scaled by its row; its column's scale and bias follow in one step.
+__device__ __forceinline__ float ring_i8_row(unsigned sum, float sa) { return static_cast<float>(static_cast<int>(sum)) * sa; }
+// eight columns' scales of B
+__device__ __forceinline__ void ring_i8_scales(const float* sb, float (&f)[8]) {
+  const float4 lo = *reinterpret_cast<const float4*>(sb), hi = *reinterpret_cast<const float4*>(sb + 4);
+  f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w; f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+}
 
 // a / d with the inverse of d that RingGrid has beside it: the product's high half falls short by one at most
 __device__ __forceinline__ int ring_div(int a, int d, unsigned inv, int& rest) {
@@ -185,8 +200,9 @@ __device__ __forceinline__ void ring_place(const RingGrid& w, int block, bool sp
 }
 
 // One output tile (of one K split): that of workgroup `block` of the grid w.
-// EPIS: bit mask of the epilogue kinds the instantiation carries; CS: column sums of a K-slow A (GemmDesc::colsum); WIDE: see ring_off.
-template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE>
+// EPIS: bit mask of the epilogue kinds the instantiation carries; CS: column sums of a K-slow A (GemmDesc::colsum); WIDE: see ring_off;
+// I8: operands of 8-bit integers (ecospa_gemm_i8).
+template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE, bool I8 = false>
 __device__ __forceinline__ void ring_tile(const GemmDesc& d, const RingGrid& w, int block) {
   constexpr int WTM = BM / 2, WTN = BN / 2, FM = WTM / 16, FN = WTN / 16, S = RING_BK / 32, NM = FM * FN, NR = FM + FN;
   constexpr int STAGE = (BM + BN) * RING_BK;
@@ -341,7 +357,8 @@ __device__ __forceinline__ void ring_tile(const GemmDesc& d, const RingGrid& w, 
       ring_for<0, NM>([&](auto m_) __attribute__((always_inline)) {
         constexpr int m = decltype(m_)::value, i = m / FN, j = m % FN;
         // B's fragment first: the accumulators then hold four consecutive columns of one row (see the epilogue)
-        ring_mfma(acc[i][j], ring_val<TB>(fb[cur][j]), ring_val<TA>(fa[cur][i]));
+        if constexpr (I8) ring_mfma_i8<(NM >= 48)>(acc[i][j], ring_val<TB>(fb[cur][j]), ring_val<TA>(fa[cur][i]));
+        else ring_mfma(acc[i][j], ring_val<TB>(fb[cur][j]), ring_val<TA>(fa[cur][i]));
         __builtin_amdgcn_sched_barrier(0);
         constexpr int R0 = m < RSLOTS ? m * NR / RSLOTS : NR, R1 = m < RSLOTS ? (m + 1) * NR / RSLOTS : NR;
         ring_for<R0, R1>([&](auto f_) __attribute__((always_inline)) {
@@ -402,16 +419,30 @@ __device__ __forceinline__ void ring_tile(const GemmDesc& d, const RingGrid& w, 
   // neighbouring column blocks swap their odd and even lane groups, so that a lane holds 8 consecutive columns (16-byte stores,
   // 64 bytes per row and instruction; staging the tile through LDS instead costs 4 us more on a 256x256 tile).
   const int mw = m0 + wm * WTM + l16;
+  float sa[I8 ? FM : 1], sb[I8 ? JP : 1][8];
+  if constexpr (I8) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i) sa[i] = gemm_i8_sa(d.epi)[min(mw + i * 16, d.M - 1)];
+#pragma unroll
+    for (int jp = 0; jp < JP; ++jp) ring_i8_scales(gemm_i8_sb(d.epi) + min(nw + jp * 32, d.N - 8), sb[jp]);
+  }
   auto vals = [&](auto i_, auto jp_, float (&v)[8]) __attribute__((always_inline)) {
     constexpr int i = decltype(i_)::value, jp = decltype(jp_)::value;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][2 * jp][r]), __float_as_uint(acc[i][2 * jp + 1][r]), false, false);
-      v[r] = __uint_as_float(p[0]);
-      v[4 + r] = __uint_as_float(p[1]);
+      v[r] = I8 ? ring_i8_row(p[0], sa[I8 ? i : 0]) : __uint_as_float(p[0]);
+      v[4 + r] = I8 ? ring_i8_row(p[1], sa[I8 ? i : 0]) : __uint_as_float(p[1]);
+    }
+    if constexpr (I8) {
+      float b[8];
+      if (has_bias) unpack8(braw[jp], b);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[q] = __builtin_fmaf(v[q], sb[jp][q], has_bias ? b[q] : -0.f);
     }
   };
-  if (d.splits > 1) {
+  if constexpr (I8 && !BIAS_EARLY) load_bias();
+  if (!I8 && d.splits > 1) {
     float* part = d.partial + static_cast<long long>(zsplit) * d.M * d.N;
     ring_for<0, FM>([&](auto i_) __attribute__((always_inline)) {
       const int m = mw + decltype(i_)::value * 16;
@@ -428,9 +459,9 @@ __device__ __forceinline__ void ring_tile(const GemmDesc& d, const RingGrid& w, 
     });
     return;
   }
-  if constexpr (!BIAS_EARLY) load_bias();
+  if constexpr (!I8 && !BIAS_EARLY) load_bias();
   auto add_bias = [&](int jp, float (&v)[8]) __attribute__((always_inline)) {
-    if (has_bias) {
+    if (!I8 && has_bias) {
       float b[8];
       unpack8(braw[jp], b);
 #pragma unroll
@@ -586,21 +617,21 @@ __device__ __forceinline__ void ring_tile(const GemmDesc& d, const RingGrid& w, 
   });
 }
 
-template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE = false>
+template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE = false, bool I8 = false>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void gemm_bf16_ring_kernel(const RingGrid w, const GemmDesc d) {
-  ring_tile<BM, BN, NS, TA, TB, CS, EPIS, WIDE>(d, w, blockIdx.x);
+  ring_tile<BM, BN, NS, TA, TB, CS, EPIS, WIDE, I8>(d, w, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------------------------
 // launch
-template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE = false>
+template <int BM, int BN, int NS, bool TA, bool TB, bool CS, int EPIS, bool WIDE = false, bool I8 = false>
 static hipError_t ring_launch_shape(ecospa_ctx* ctx, const GemmDesc& d, int k_chunk) {
   const int splits = d.splits > 1 ? d.splits : 1;
   const RingGrid w = gemm_ring_grid(d.M, d.N, BM, BN, splits, k_chunk);
   constexpr int lds_bytes = NS * (BM + BN) * RING_BK * static_cast<int>(sizeof(bf16_t));
   static_assert(lds_bytes <= 160 * 1024, "LDS of a compute unit");
-  auto kern = gemm_bf16_ring_kernel<BM, BN, NS, TA, TB, CS, EPIS, WIDE>;
+  auto kern = gemm_bf16_ring_kernel<BM, BN, NS, TA, TB, CS, EPIS, WIDE, I8>;
   static LdsAttrOnce attr_once;
   if (lds_bytes > 64 * 1024) {
     const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), lds_bytes);

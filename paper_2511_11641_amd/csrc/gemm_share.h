@@ -31,7 +31,8 @@ template <int N> __device__ __forceinline__ void share_wait_vm() {
   asm volatile("" ::: "memory");
 }
 
-template <int BM, int BN, int W, int D>
+// I8: operands of 8-bit integers (ecospa_gemm_i8).
+template <int BM, int BN, int W, int D, bool I8 = false>
 __global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4)))
 void gemm_bf16_share_kernel(const RingGrid w, const GemmDesc d) {
   typedef ShareTile<BM, BN, W, D> S;
@@ -90,6 +91,7 @@ void gemm_bf16_share_kernel(const RingGrid w, const GemmDesc d) {
   const bool finishes = wave * PPW < S::PAIRS, has_bias = d.epi.bias != nullptr && d.epi.kind != EPI_DACT && d.epi.kind != EPI_DSWIGLU;
   uint4 braw[PPW];
   EpiSide side[PPW];
+  float sa[I8 ? PPW : 1], sb[I8 ? PPW : 1][8];
   if (finishes) {
 #pragma unroll
     for (int q = 0; q < PPW; ++q) {
@@ -98,6 +100,10 @@ void gemm_bf16_share_kernel(const RingGrid w, const GemmDesc d) {
       m = min(m, d.M - 1);
       c = min(c, d.N - 8);
       if (has_bias) braw[q] = *reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(d.epi.bias) + c);
+      if constexpr (I8) {
+        sa[q] = gemm_i8_sa(d.epi)[m];
+        ring_i8_scales(gemm_i8_sb(d.epi) + c, sb[q]);
+      }
       if (d.epi.kind == EPI_ROPE) epi_side_load_k<EPI_ROPE>(d.epi, m, c, side[q]);
       else if (d.epi.kind == EPI_DACT) epi_side_load_k<EPI_DACT>(d.epi, m, c, side[q]);
       else if (d.epi.kind == EPI_DSWIGLU) epi_side_load_k<EPI_DSWIGLU>(d.epi, m, c, side[q]);
@@ -163,7 +169,10 @@ void gemm_bf16_share_kernel(const RingGrid w, const GemmDesc d) {
       for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fb[s][j]), __builtin_bit_cast(bf16x8_t, fa[s][i]), acc[i][j], 0, 0, 0);
+          if constexpr (I8)
+            acc[i][j] = __builtin_bit_cast(ring_f4, __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(ring_i4, fb[s][j]), __builtin_bit_cast(ring_i4, fa[s][i]), __builtin_bit_cast(ring_i4, acc[i][j]), 0, 0, 0));
+          else
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, fb[s][j]), __builtin_bit_cast(bf16x8_t, fa[s][i]), acc[i][j], 0, 0, 0);
   };
   int i = 0, buf = 0;
   auto next = [&]() __attribute__((always_inline)) { ++i; buf = buf + 1 == D ? 0 : buf + 1; };
@@ -198,30 +207,40 @@ void gemm_bf16_share_kernel(const RingGrid w, const GemmDesc d) {
       }
 #pragma unroll
       for (int z = 1; z < W; ++z) {
-        x[0].x += x[z].x; x[0].y += x[z].y; x[0].z += x[z].z; x[0].w += x[z].w;
-        y[0].x += y[z].x; y[0].y += y[z].y; y[0].z += y[z].z; y[0].w += y[z].w;
+        if constexpr (I8) {
+          x[0] = __builtin_bit_cast(float4, __builtin_bit_cast(ring_i4, x[0]) + __builtin_bit_cast(ring_i4, x[z]));
+          y[0] = __builtin_bit_cast(float4, __builtin_bit_cast(ring_i4, y[0]) + __builtin_bit_cast(ring_i4, y[z]));
+        } else {
+          x[0].x += x[z].x; x[0].y += x[z].y; x[0].z += x[z].z; x[0].w += x[z].w;
+          y[0].x += y[z].x; y[0].y += y[z].y; y[0].z += y[z].z; y[0].w += y[z].w;
+        }
       }
       const float xs[4] = {x[0].x, x[0].y, x[0].z, x[0].w}, ys[4] = {y[0].x, y[0].y, y[0].z, y[0].w};
       float v[8], b[8];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {       // odd and even lane groups swap: a lane then holds 8 consecutive columns
         const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(xs[r]), __float_as_uint(ys[r]), false, false);
-        v[r] = __uint_as_float(p[0]);
-        v[4 + r] = __uint_as_float(p[1]);
+        v[r] = I8 ? ring_i8_row(p[0], sa[I8 ? q : 0]) : __uint_as_float(p[0]);
+        v[4 + r] = I8 ? ring_i8_row(p[1], sa[I8 ? q : 0]) : __uint_as_float(p[1]);
       }
       int m, c;
       place(q, m, c);
       if (has_bias) unpack8(braw[q], b);
-      if (m < d.M && c < d.N) epi_apply_vec8_k<KIND>(d.epi, m, c, v, has_bias, b, side[q]);
+      if constexpr (I8) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = __builtin_fmaf(v[r], sb[q][r], has_bias ? b[r] : -0.f);
+      }
+      if constexpr (!I8 || ((GEMM_EPIS_I8 >> KIND) & 1))
+        if (m < d.M && c < d.N) epi_apply_vec8_k<KIND>(d.epi, m, c, v, !I8 && has_bias, b, side[q]);
     }
   });
 }
 
-template <int BM, int BN, int W, int D>
+template <int BM, int BN, int W, int D, bool I8 = false>
 static hipError_t share_launch_shape(ecospa_ctx* ctx, const GemmDesc& d) {
   const RingGrid w = gemm_ring_grid(d.M, d.N, BM, BN, 1, 0);
   constexpr int lds_bytes = W * ShareTile<BM, BN, W, D>::AREA;
-  auto kern = gemm_bf16_share_kernel<BM, BN, W, D>;
+  auto kern = gemm_bf16_share_kernel<BM, BN, W, D, I8>;
   static LdsAttrOnce attr_once;
   if (lds_bytes > 64 * 1024) {
     const hipError_t e = attr_once.ensure(reinterpret_cast<const void*>(kern), lds_bytes);
