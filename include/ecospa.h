@@ -621,6 +621,70 @@ int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype, const void
 int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, long long lda, const float* sa, const void* B, long long ldb,
                        const float* sb, const void* bias, int act, void* C, long long ldc);
 
+/* ------------------------------------------------------------------------------------------
+ * Own caches in 8-bit floats.  As ecospa_cache, but keys and values are codes of the OCP e4m3 type (1 sign, 4 exponent, 3 mantissa bits; largest 448, no infinity) with
+ * an fp32 scale for each block of `block` consecutive rows and key/value head: a key is k_scale[b, g, row / block] * code.  Half the bytes of bf16 to
+ * keep and to read.  There is no shared prefix in it: attention over one (ecospa_prefix_attn of a cache without own keys) is joined in by the call.
+ *
+ * ecospa_quant_cache: strides in elements (bytes), multiples of 16, at most 2^25 - 1 between rows; k, v 16-byte aligned; k_scale, v_scale dense
+ * float[B, h_kv, ceil(cap / block)]; block 16, 32, 64 or 128; the other fields as ecospa_cache's.  Rows at and beyond lens[b], and scales of blocks without a row, are never
+ * read, but own_max bounds lens as there.
+ * Common errors, before any launch: ERR_NULL; ERR_SHAPE (as ecospa_cache's, block, B * h_kv > 65535); ERR_ALIGN; ERR_WORKSPACE.
+ *
+ * ecospa_quant_cache_append: as ecospa_cache_append (queries, positions, tables, tokens without a place).  Keys (turned, rounded to bf16) and values are stored as value / scale,
+ * rounded to nearest even.  A block's scale is the least power of two, 2^-100 or more, that keeps its rows within 448, and does not fall while it has earlier rows; if it rises
+ * for a new row, the codes of the earlier ones are brought to it (exact but for those below the type's normal range).  A block that the new rows begin
+ * starts anew.  Infinite elements are stored as NaN; NaN plays no part in the scale.  Earlier rows of a block belong to tokens in front of the call's: tokens are
+ * appended in order.
+ *
+ * ecospa_quant_cache_attn: as ecospa_prefix_attn over the own keys: query (b, t) sees the keys j < lens[b] - L + 1 + t.  o_in (bf16 [B*L, h*kp_vo], ld_oi) and lse_in
+ * (float[B, h, L]): the result of attention over other keys - a shared prefix - which is joined in as ecospa_prefix_attn would have: o and lse are those over
+ * all the keys; rows of o_in with lse_in = -inf are not read (both NULL: none; o may be o_in with the same ld, lse may be lse_in).  A query that sees no key has o = 0 and
+ * lse = -inf; NaN and +inf scores as there.  Probabilities (times the value's scale) enter their product with the codes rounded to bf16; lse comes from the unrounded ones.
+ * Workspace: ecospa_quant_cache_attn_workspace_bytes (host-only query; 0 when none is needed or on bad input). */
+typedef struct {
+  int B, h, h_kv, kp_qk, kp_vo;
+  int cap, own_max;
+  int block;                 /* rows that share a scale                                        */
+  float scale;               /* softmax scale                                                  */
+  void *k, *v;               /* e4m3 codes                                                     */
+  long long k_sb, k_sh, k_st, v_sb, v_sh, v_st;
+  float *k_scale, *v_scale;
+  const int* lens;           /* device int32[B]                                                */
+} ecospa_quant_cache;
+int ecospa_quant_cache_append(ecospa_ctx* ctx, const ecospa_quant_cache* cache /*host*/, int L, const void* qkv, long long ld_qkv, const int* pos,
+                              const float* rope_cos, const float* rope_sin, int L_tab, void* q, long long ld_q);
+size_t ecospa_quant_cache_attn_workspace_bytes(const ecospa_quant_cache* cache /*host*/, int L);
+int ecospa_quant_cache_attn(ecospa_ctx* ctx, const ecospa_quant_cache* cache /*host*/, int L, const void* q, long long ld_q, const void* o_in,
+                            long long ld_oi, const float* lse_in, void* o, long long ld_o, float* lse);
+
+/* ------------------------------------------------------------------------------------------
+ * A token drawn for every row of logits by a given random number.  For row b with logits x (after ecospa_logits_process; -inf: masked) and T = temperature[b], tokens are
+ * ordered by logit, the larger first, equal ones by index, and weigh w_v = exp((x_v - max x) / T).  Kept is the shortest of the leading parts that
+ *   hold top_k[b] tokens (top_k[b] < 1: all),
+ *   are the first whose weight is at least top_p[b] of that of the top_k[b] tokens (top_p[b] >= 1: all of them; at least one token),
+ *   hold the tokens with w_v >= min_p[b] (of the best one's weight; min_p[b] > 1 counts as 1).
+ * token[b] is the first token v, in the order of the vocabulary, with  sum of the kept w up to and with v  >  u[b] * sum of all kept w  (u in [0, 1); below: 0, beyond: the last kept
+ * token), prob[b] (float[B], NULL: not wanted) its share of the kept weight.  T = 0, negative or NaN: the best token, probability 1.  A token of +inf shares its
+ * row with others of +inf alone.  A row of -inf and NaN alone has token -1 and prob 0; NaN weighs nothing.  NaN in top_p and min_p counts as not given, in u as 0.
+ * Weights are held as whole numbers of 2^-42 of the best one's binade, so sums do not depend on an order and results repeat bit for bit; tokens below that weigh nothing.
+ * Parameter arrays (device, [B]) may be NULL: T = 1, no top_k, top_p or min_p.  dtype ECOSPA_F32 or ECOSPA_BF16.
+ * Errors: ERR_NULL (logits, u, token); ERR_DTYPE; ERR_SHAPE (B, V < 1, B > 65535, V > 2^20, ld < V); ERR_ALIGN (logits 16 bytes, ld % 8);
+ * ERR_WORKSPACE (ecospa_sample_workspace_bytes). */
+typedef struct {
+  int B, V, dtype;
+  const void* logits;
+  long long ld;
+  const float* u;            /* [B] random numbers                                             */
+  const float* temperature;  /* [B] or NULL, as the following                                  */
+  const int* top_k;
+  const float *top_p, *min_p;
+  int* token;                /* int32[B]                                                       */
+  float* prob;               /* float[B] or NULL                                               */
+} ecospa_sample_args;
+size_t ecospa_sample_workspace_bytes(int B, int V);
+int ecospa_sample(ecospa_ctx* ctx, const ecospa_sample_args* args /*host*/);
+
 #ifdef __cplusplus
 }
 #endif

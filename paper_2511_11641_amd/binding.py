@@ -36,6 +36,8 @@ EXPORTS = (
     "ecospa_cache_append", "ecospa_prefix_attn", "ecospa_prefix_attn_workspace_bytes", "ecospa_cache_evict",
     "ecospa_logits_process", "ecospa_logits_workspace_bytes",
     "ecospa_quant_rows", "ecospa_contract_quant",
+    "ecospa_quant_cache_append", "ecospa_quant_cache_attn", "ecospa_quant_cache_attn_workspace_bytes",
+    "ecospa_sample", "ecospa_sample_workspace_bytes",
 )
 NORM_RMS, NORM_LAYER = 0, 1
 
@@ -118,6 +120,19 @@ class Logits(C.Structure):
                 ("n_bias", C.c_int), ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("temperature", C.c_void_p),
                 ("bias_ids", C.c_void_p), ("bias", C.c_void_p), ("mask", C.c_void_p), ("mask_row", C.c_void_p), ("ld_mask", C.c_longlong),
                 ("n_masks", C.c_int), ("pick", C.c_void_p), ("lse", C.c_void_p)]
+
+
+class QuantCacheDesc(C.Structure):
+    _fields_ = [("B", C.c_int), ("h", C.c_int), ("h_kv", C.c_int), ("kp_qk", C.c_int), ("kp_vo", C.c_int), ("cap", C.c_int), ("own_max", C.c_int),
+                ("block", C.c_int), ("scale", C.c_float), ("k", C.c_void_p), ("v", C.c_void_p), ("k_sb", C.c_longlong), ("k_sh", C.c_longlong),
+                ("k_st", C.c_longlong), ("v_sb", C.c_longlong), ("v_sh", C.c_longlong), ("v_st", C.c_longlong), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("lens", C.c_void_p)]
+
+
+class SampleArgs(C.Structure):
+    _fields_ = [("B", C.c_int), ("V", C.c_int), ("dtype", C.c_int), ("logits", C.c_void_p), ("ld", C.c_longlong), ("u", C.c_void_p),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("token", C.c_void_p),
+                ("prob", C.c_void_p)]
 
 
 class Grads(C.Structure):
@@ -234,6 +249,16 @@ def load() -> C.CDLL:
     lib.ecospa_quant_rows.restype = ci
     lib.ecospa_contract_quant.argtypes = [vp, ci, ci, ci, vp, ll, vp, vp, ll, vp, vp, ci, vp, ll]
     lib.ecospa_contract_quant.restype = ci
+    lib.ecospa_quant_cache_append.argtypes = [vp, C.POINTER(QuantCacheDesc), ci, vp, ll, vp, vp, vp, ci, vp, ll]
+    lib.ecospa_quant_cache_append.restype = ci
+    lib.ecospa_quant_cache_attn.argtypes = [vp, C.POINTER(QuantCacheDesc), ci, vp, ll, vp, ll, vp, vp, ll, vp]
+    lib.ecospa_quant_cache_attn.restype = ci
+    lib.ecospa_quant_cache_attn_workspace_bytes.argtypes = [C.POINTER(QuantCacheDesc), ci]
+    lib.ecospa_quant_cache_attn_workspace_bytes.restype = sz
+    lib.ecospa_sample.argtypes = [vp, C.POINTER(SampleArgs)]
+    lib.ecospa_sample.restype = ci
+    lib.ecospa_sample_workspace_bytes.argtypes = [ci, ci]
+    lib.ecospa_sample_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -311,6 +336,38 @@ class KvCache:
         return self._need[key]
 
 
+class QuantCache:
+    """A batch's own key/value caches in 8-bit floats on compact heads (ecospa_quant_cache).
+
+    k: [B, h_kv, cap, kp_qk], v: [B, h_kv, cap, kp_vo] (float8_e4m3fn, last dim dense, other strides free, multiples of 16); k_scale, v_scale: float32
+    [B, h_kv, ceil(cap / block)], dense; lens: int32 [B]; h query heads; scale: the softmax scale; block: rows that share a scale; own_max as
+    :class:`KvCache`'s.  The object keeps the tensors alive; their contents are read when the kernels run."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, lens: torch.Tensor, h: int, scale: float,
+                 block: int, own_max: Optional[int] = None):
+        (Bsz, h_kv, cap, kq), (k_sb, k_sh, k_st, k_unit) = k.shape, k.stride()
+        (vB, vh, vcap, kv), (v_sb, v_sh, v_st, v_unit) = v.shape, v.stride()
+        f8 = torch.float8_e4m3fn
+        if (vB, vh, vcap) != (Bsz, h_kv, cap) or k.dtype != f8 or v.dtype != f8 or k_unit != 1 or v_unit != 1 or block < 1:
+            raise ValueError(f"expected {f8} caches of equal length, got {k.dtype} {tuple(k.shape)} and {v.dtype} {tuple(v.shape)}, block {block}")
+        self.k, self.v, self.k_scale, self.v_scale, self.lens = k, v, k_scale, v_scale, lens
+        self.B, self.h, self.h_kv, self.cap, self.kq, self.kv, self.scale, self.block = Bsz, h, h_kv, cap, kq, kv, scale, block
+        self.nq, self.no, self.nqkv = h * kq, h * kv, (h + h_kv) * kq + h_kv * kv
+        n = Bsz * h_kv * ((cap + block - 1) // block)
+        self.desc = QuantCacheDesc(Bsz, h, h_kv, kq, kv, cap, cap if own_max is None else own_max, block, scale, k.data_ptr(), v.data_ptr(), k_sb, k_sh, k_st,
+                                   v_sb, v_sh, v_st, _dense(k_scale, torch.float32, n), _dense(v_scale, torch.float32, n), _dense(lens, torch.int32, Bsz))
+        self._ref = C.byref(self.desc)
+        self._need = {}
+
+    own_max = KvCache.own_max
+
+    def workspace_bytes(self, L: int) -> int:
+        key = (L, self.desc.own_max)
+        if key not in self._need:
+            self._need[key] = load().ecospa_quant_cache_attn_workspace_bytes(self._ref, L)
+        return self._need[key]
+
+
 class Context:
     """One ecospa_ctx on the current torch stream, with a torch-owned workspace that grows on demand."""
 
@@ -326,6 +383,7 @@ class Context:
         self.h = h
         self._ws: Optional[torch.Tensor] = None
         self._logits_need: dict = {}      # workspace of a (B, V)
+        self._sample_need: dict = {}
 
     def __del__(self):
         try:
@@ -778,6 +836,59 @@ class Context:
                    ids_ptr, bias_ptr, mask_ptr, _dense(mask_row, i32, Bsz), ld_mask, n_masks, _dense(pick, i32, Bsz), _dense(lse, f32, Bsz))
         self._check(self.lib.ecospa_logits_process(self.h, C.byref(a)), "ecospa_logits_process")
         return pick, lse
+
+    def ecospa_sample(self, logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                      top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, token: Optional[torch.Tensor] = None,
+                      prob: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """A token int32 [B] for every row of logits [B, V], drawn by u float32 [B] in [0, 1) from what temperature, top_k (int32), top_p and min_p
+        leave (each [B] or None); prob float32 [B]: its probability there.  No token to draw: -1."""
+        (Bsz, V), (ld, unit) = logits.shape, logits.stride()
+        f32, i32 = torch.float32, torch.int32
+        if unit != 1:
+            raise ValueError(f"expected dense rows of logits, got strides {logits.stride()}")
+        token = torch.empty(Bsz, dtype=i32, device=logits.device) if token is None else token
+        need = self._sample_need.get((Bsz, V))
+        if need is None:
+            need = self._sample_need[Bsz, V] = self.lib.ecospa_sample_workspace_bytes(Bsz, V)
+        self.reserve(need)
+        a = SampleArgs(Bsz, V, dtype_code(logits.dtype), logits.data_ptr(), ld, _dense(u, f32, Bsz), _dense(temperature, f32, Bsz), _dense(top_k, i32, Bsz),
+                       _dense(top_p, f32, Bsz), _dense(min_p, f32, Bsz), _dense(token, i32, Bsz), _dense(prob, f32, Bsz))
+        self._check(self.lib.ecospa_sample(self.h, C.byref(a)), "ecospa_sample")
+        return token
+
+    # ---- caches in 8-bit floats ------------------------------------------------------------------
+    def ecospa_quant_cache_append(self, cache: QuantCache, qkv: torch.Tensor, pos: Optional[torch.Tensor] = None, rope=None,
+                                  q: Optional[torch.Tensor] = None):
+        """:meth:`ecospa_cache_append` into caches of 8-bit floats: the new tokens become the last L rows, block scales rise where they have to."""
+        T, ld = self._rows(qkv, cache.nqkv)
+        Tq, ldq = (T, 0) if q is None else self._rows(q, cache.nq)
+        if T % cache.B or Tq != T:
+            raise ValueError(f"{T} rows (queries {Tq}) for {cache.B} requests")
+        cos_ptr = sin_ptr = None
+        tab = 0
+        if rope is not None:
+            cos, sin = rope
+            tab = cos.shape[1]
+            n = cache.h_kv * tab * (cache.kq // 2)
+            cos_ptr, sin_ptr = _dense(cos, torch.float32, n), _dense(sin, torch.float32, n)
+        self._check(self.lib.ecospa_quant_cache_append(self.h, cache._ref, T // cache.B, qkv.data_ptr(), ld, _dense(pos, torch.int32, cache.B), cos_ptr,
+                                                       sin_ptr, tab, _ptr(q), ldq), "ecospa_quant_cache_append")
+
+    def ecospa_quant_cache_attn(self, cache: QuantCache, q: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                                o_in: Optional[torch.Tensor] = None, lse_in: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """o [B*L, h * kp_vo] = attention of the new tokens' queries q [B*L, h * kp_qk] over the own caches; o_in (as o) and lse_in float32
+        [B, h, L]: the result over other keys, joined in; lse float32 [B, h, L]: over all of them."""
+        T, ldq = self._rows(q, cache.nq)
+        To, ldo = self._rows(o, cache.no)
+        Ti, ldi = (T, 0) if o_in is None else self._rows(o_in, cache.no)
+        L = T // cache.B
+        if T % cache.B or To != T or Ti != T:
+            raise ValueError(f"{T} rows (outputs {To}, {Ti}) for {cache.B} requests")
+        self.reserve(cache.workspace_bytes(L))
+        n = T * cache.h
+        self._check(self.lib.ecospa_quant_cache_attn(self.h, cache._ref, L, q.data_ptr(), ldq, _ptr(o_in), ldi, _dense(lse_in, torch.float32, n), o.data_ptr(),
+                                                     ldo, _dense(lse, torch.float32, n)), "ecospa_quant_cache_attn")
+        return o
 
     # ---- products in 8-bit integers --------------------------------------------------------------
     def ecospa_quant_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
