@@ -21,8 +21,9 @@ typedef unsigned qa_uintx4 __attribute__((ext_vector_type(4)));
 #define QA_RESCALE 8.0f        // growth of a row's maximum, in binades, that brings its sums to the new one
 #define QA_LN2 0.6931471805599453f
 
+// two codes times the power of two below `scale` (the instruction looks at its exponent alone)
 template <bool HIGH>
-__device__ __forceinline__ unsigned qa_pair(unsigned codes) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.0f, HIGH)); }
+__device__ __forceinline__ unsigned qa_pair(unsigned codes, float scale = 1.0f) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HIGH)); }
 // eight codes of a key to a fragment
 __device__ __forceinline__ qa_bf16x8 qa_frag(unsigned lo, unsigned hi) {
   return __builtin_bit_cast(qa_bf16x8, qa_uintx4{qa_pair<false>(lo), qa_pair<true>(lo), qa_pair<false>(hi), qa_pair<true>(hi)});
@@ -162,12 +163,15 @@ void quant_attn_kernel(const QuantAttnArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const unsigned two = __builtin_amdgcn_perm(x.v[2 * e + 1][f >> 2], x.v[2 * e][f >> 2], f & 2 ? 0x07030602u : 0x05010400u);
-        w[0][e] = qa_pair<false>(two);
-        w[1][e] = qa_pair<true>(two);
+        w[0][e] = qa_pair<false>(two, x.vs[e >> 1]);
+        w[1][e] = qa_pair<true>(two, x.vs[e >> 1]);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) vf[f + u] = __builtin_bit_cast(qa_bf16x8, qa_uintx4{w[u][0], w[u][1], w[u][2], w[u][3]});
     }
+    // what the exponents of the values' scales leave: 1 for powers of two, which is what an append writes
+    const float rest[2] = {__uint_as_float((__float_as_uint(x.vs[0]) & 0x807fffffu) | 0x3f800000u), __uint_as_float((__float_as_uint(x.vs[1]) & 0x807fffffu) | 0x3f800000u)};
+    const bool powers = rest[0] == 1.f && rest[1] == 1.f;
     qa_floatx4 s[T][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -182,31 +186,38 @@ void quant_attn_kernel(const QuantAttnArgs a) {
       }
     }
     const float by[2] = {x.ks[0] * a.scale_log2, x.ks[1] * a.scale_log2};
-    const bool masked = c * 32 + 32 > sees_first;
+    if (c * 32 + 32 > sees_first) {
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int key = c * 32 + 16 * (e >> 2) + 4 * g + (e & 3);
+          s[t][e >> 2][e & 3] = key < sees[t] && key < key1 ? s[t][e >> 2][e & 3] : -INFINITY;
+        }
+    }
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[t][e >> 2][e & 3] * by[e >> 2];
-      if (masked) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) p[e] = c * 32 + 16 * (e >> 2) + 4 * g + (e & 3) < sees[t] && c * 32 + 16 * (e >> 2) + 4 * g + (e & 3) < key1 ? p[e] : -INFINITY;
-      }
-      const float top = qa_max4(fmaxf(fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3])), fmaxf(fmaxf(p[4], p[5]), fmaxf(p[6], p[7]))));
+      // the lane's own largest: the row's reference has to be near it, not equal to it, so the lanes of a row agree on a new one only where it falls behind
+      const float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])) * by[0], fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])) * by[1]);
       if (__any(top > m[t] + QA_RESCALE)) {
-        const float up = fmaxf(m[t], top), f0 = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - up);
+        const float up = fmaxf(m[t], qa_max4(top)), f0 = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - up);
         m[t] = up;
         l[t] = l[t] == 0.f ? 0.f : l[t] * f0;
 #pragma unroll
         for (int f = 0; f < W; ++f) o[t][f] *= f0;
       }
       const float ref = m[t] == -INFINITY ? 0.f : m[t];
+      float p[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 2][e & 3], by[e >> 2], -ref));
       l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      if (!powers) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] *= rest[e >> 2];
+      }
       qa_floatx8 w;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = p[e] * x.vs[e >> 2];
+      for (int e = 0; e < 8; ++e) w[e] = p[e];
       const qa_bf16x8 pf = __builtin_convertvector(w, qa_bf16x8);
 #pragma unroll
       for (int f = 0; f < W; ++f) o[t][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[f], pf, o[t][f], 0, 0, 0);
@@ -214,23 +225,31 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   };
   const int end = (key1 + 31) >> 5;      // groups up to here; key0 is a multiple of 128
   int c = (key0 >> 5) + wave;
-  if (T == 4 && W == 8) {      // no registers for a second group
-    for (; c < end; c += WAVES) {
-      QaRaw<KQ, W> x;
-      load(c, x);
-      step(c, x);
-    }
-  } else if (c < end) {
-    // the next group is on its way while one is computed; two sets of registers in turn, so that none is moved
-    QaRaw<KQ, W> x, y;
+  // The next group is on its way while one is computed, in two sets of registers in turn.  Behind the last one it is asked for again: a load that may or may not
+  // have been issued would be waited for together with those in front of it (attention of prompts: ).
+  if (c < end) {
+    const int last = c + (end - 1 - c) / WAVES * WAVES;
+    QaRaw<KQ, W> x;
     load(c, x);
-    for (;; c += 2 * WAVES) {
-      if (c + WAVES < end) load(c + WAVES, y);
-      step(c, x);
-      if (c + WAVES >= end) break;
-      if (c + 2 * WAVES < end) load(c + 2 * WAVES, x);
-      step(c + WAVES, y);
-      if (c + 2 * WAVES >= end) break;
+    if constexpr (T == 4 && W == 8) {      // no registers for a second group
+      for (;;) {
+        step(c, x);
+        if (c == last) break;
+        c += WAVES;
+        load(c, x);
+      }
+    } else {
+      QaRaw<KQ, W> y;
+      for (;;) {
+        load(min(c + WAVES, last), y);
+        step(c, x);
+        if (c == last) break;
+        c += WAVES;
+        load(min(c + WAVES, last), x);
+        step(c, y);
+        if (c == last) break;
+        c += WAVES;
+      }
     }
   }
 

@@ -16,12 +16,28 @@ __global__ __launch_bounds__(256) void quant_attn_join_kernel(const QuantAttnArg
   const float ref = top == -INFINITY ? 0.f : top;
   float all = 0.f, v0 = 0.f, v1 = 0.f;
   const int d0 = min(lane, a.kv - 1), d1 = min(lane + 64, a.kv - 1);
-  for (int i = 0; i < a.pieces; ++i) {
-    const float* const p = part + i * next;
-    const float m = p[pitch - 2], l = p[pitch - 1], f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - ref);
-    all += l == 0.f ? 0.f : l * f;
-    v0 += l == 0.f ? 0.f : p[d0] * f;
-    v1 += l == 0.f ? 0.f : p[d1] * f;
+  // a lane a piece for its factor, then eight pieces' values on their way together
+  for (int i0 = 0; i0 < a.pieces; i0 += 64) {
+    const int i = i0 + lane;
+    const float l = i < a.pieces ? part[i * next + pitch - 1] : 0.f, f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(part[i * next + pitch - 2] - ref);
+    all += wave_sum(l == 0.f ? 0.f : l * f);
+    const int here = min(a.pieces - i0, 64);
+    for (int j0 = 0; j0 < here; j0 += 8) {
+      float x0[8], x1[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float* const p = part + (i0 + min(j0 + j, here - 1)) * next;
+        x0[j] = p[d0];
+        x1[j] = a.kv > 64 ? p[d1] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float fj = __shfl(f, min(j0 + j, 63), 64);
+        const bool on = j0 + j < here && fj != 0.f;      // a piece without keys has no values (NaN factors are kept)
+        v0 += on ? x0[j] * fj : 0.f;
+        v1 += on ? x1[j] * fj : 0.f;
+      }
+    }
   }
   const int tok = row / a.g, head = hk * a.g + row - tok * a.g;
   const long long flat = (static_cast<long long>(b) * a.h + head) * a.L + tok, orow = static_cast<long long>(b) * a.L + tok;
@@ -57,7 +73,8 @@ static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {
   p.row_blocks = (rows + 16 * p.T - 1) / (16 * p.T);
   const long long items = static_cast<long long>(c->B) * c->h_kv * p.row_blocks;
   const int most = (c->own_max + 255) / 256;      // pieces of at least 256 keys
-  long long want = items >= 4096 ? 1 : (4096 + items - 1) / items;
+  const int fill = p.T == 4 ? 1024 : 4096;
+  long long want = items >= fill ? 1 : (fill + items - 1) / items;
   if (want > most) want = most;
   if (want < 1) want = 1;
   p.piece_keys = static_cast<int>((c->own_max + want - 1) / want);
