@@ -66,7 +66,7 @@ __device__ __forceinline__ void qa_finish_row(float& m, float& l, float& in, con
 }
 
 template <int T, int KQ, int W>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T == 1 ? (W == 8 ? 2 : 3) : 1, 8)))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T == 1 && W < 8 ? (KQ < 4 ? 4 : 3) : 2)))
 void quant_attn_kernel(const QuantAttnArgs a) {
   constexpr int WAVES = 4, ROWS = 16 * T, KV = 16 * W, PITCH = KV + 4;
   __shared__ __attribute__((aligned(16))) float lds_o[WAVES][16][PITCH];
@@ -107,28 +107,37 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   }
   const unsigned vd = W * l16 < a.kv ? W * l16 : 0, kst = static_cast<unsigned>(a.k_st), vst = static_cast<unsigned>(a.v_st);
 
+  // a lane's rows of a group; in the last one of a piece those beyond the last key repeat it: nothing behind a length is read
+  unsigned koff[2], voff[8];
+  const auto aim = [&](int most) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) koff[i] = static_cast<unsigned>(min(16 * i + l16, most)) * kst;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) voff[e] = static_cast<unsigned>(min(16 * (e >> 2) + 4 * g + (e & 3), most)) * vst + vd;
+  };
+  aim(31);
   const auto load = [&](int c, QaRaw<KQ, W>& x) __attribute__((always_inline)) {
-    const int k0 = c * 32, most = key1 - 1 - k0;      // rows beyond the last key repeat it: nothing behind a length is read
+    const int k0 = c * 32;
+    if (k0 + 32 > key1) aim(key1 - 1 - k0);
     const unsigned char* const kp = kb + static_cast<long long>(k0) * a.k_st;
     const unsigned char* const vp = vb + static_cast<long long>(k0) * a.v_st;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const unsigned char* const p = kp + static_cast<unsigned>(min(16 * i + l16, most)) * kst;
 #pragma unroll
       for (int s = 0; s < KQ; s += 2) {
         if (s + 1 < KQ) {
-          const uint4 u = *reinterpret_cast<const uint4*>(p + kd[s / 2]);
+          const uint4 u = *reinterpret_cast<const uint4*>(kp + (koff[i] + kd[s / 2]));
           x.k[i][2 * s] = u.x; x.k[i][2 * s + 1] = u.y;
           x.k[i][(2 * s + 2) % (2 * KQ)] = u.z; x.k[i][(2 * s + 3) % (2 * KQ)] = u.w;
         } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(p + kd[s / 2]);
+          const uint2 u = *reinterpret_cast<const uint2*>(kp + (koff[i] + kd[s / 2]));
           x.k[i][2 * s] = u.x; x.k[i][2 * s + 1] = u.y;
         }
       }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const unsigned char* const p = vp + static_cast<unsigned>(min(16 * (e >> 2) + 4 * g + (e & 3), most)) * vst + vd;
+      const unsigned char* const p = vp + voff[e];
       if constexpr (W == 8) {
         const uint2 u = *reinterpret_cast<const uint2*>(p);
         x.v[e][0] = u.x; x.v[e][W > 4 ? 1 : 0] = u.y;
@@ -198,7 +207,10 @@ void quant_attn_kernel(const QuantAttnArgs a) {
 #pragma unroll
     for (int t = 0; t < T; ++t) {
       // the lane's own largest: the row's reference has to be near it, not equal to it, so the lanes of a row agree on a new one only where it falls behind
-      const float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])) * by[0], fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])) * by[1]);
+      float most[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most[e >> 2] = fmaxf(most[e >> 2], s[t][e >> 2][e & 3]);
+      const float top = fmaxf(most[0] * by[0], most[1] * by[1]);
       if (__any(top > m[t] + QA_RESCALE)) {
         const float up = fmaxf(m[t], qa_max4(top)), f0 = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - up);
         m[t] = up;
@@ -231,25 +243,16 @@ void quant_attn_kernel(const QuantAttnArgs a) {
     const int last = c + (end - 1 - c) / WAVES * WAVES;
     QaRaw<KQ, W> x;
     load(c, x);
-    if constexpr (T == 4 && W == 8) {      // no registers for a second group
-      for (;;) {
-        step(c, x);
-        if (c == last) break;
-        c += WAVES;
-        load(c, x);
-      }
-    } else {
-      QaRaw<KQ, W> y;
-      for (;;) {
-        load(min(c + WAVES, last), y);
-        step(c, x);
-        if (c == last) break;
-        c += WAVES;
-        load(min(c + WAVES, last), x);
-        step(c, y);
-        if (c == last) break;
-        c += WAVES;
-      }
+    QaRaw<KQ, W> y;
+    for (;;) {
+      load(min(c + WAVES, last), y);
+      step(c, x);
+      if (c == last) break;
+      c += WAVES;
+      load(min(c + WAVES, last), x);
+      step(c, y);
+      if (c == last) break;
+      c += WAVES;
     }
   }
 
@@ -314,7 +317,7 @@ static hipError_t quant_attn_launch(const QuantAttnArgs& a, hipStream_t st) {
 }
 template <int W>
 static hipError_t quant_attn_dispatch(const QuantAttnArgs& a, int T, int KQ, hipStream_t st) {
-#define QA_CASE(t, k) if (T == t && KQ == k) return quant_attn_launch<t, k, W>(a, st);
+#define QA_CASE(t, k) if constexpr (t <= quant_attn_tiles(k, W)) if (T == t && KQ == k) return quant_attn_launch<t, k, W>(a, st);
   QA_CASE(1, 1) QA_CASE(1, 2) QA_CASE(1, 3) QA_CASE(1, 4) QA_CASE(2, 1) QA_CASE(2, 2) QA_CASE(2, 3) QA_CASE(2, 4) QA_CASE(4, 1) QA_CASE(4, 2) QA_CASE(4, 3) QA_CASE(4, 4)
 #undef QA_CASE
   return hipErrorInvalidValue;

@@ -68,12 +68,12 @@ struct QuantPlan { int T, row_blocks, pieces, piece_keys, W; };
 static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {
   QuantPlan p;
   const int rows = c->h / c->h_kv * L;
-  p.T = rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
   p.W = c->kp_vo <= 32 ? 2 : (c->kp_vo <= 64 ? 4 : 8);
+  p.T = rows <= 16 ? 1 : (rows <= 32 || quant_attn_tiles((c->kp_qk + 31) / 32, p.W) == 2 ? 2 : 4);
   p.row_blocks = (rows + 16 * p.T - 1) / (16 * p.T);
   const long long items = static_cast<long long>(c->B) * c->h_kv * p.row_blocks;
   const int most = (c->own_max + 255) / 256;      // pieces of at least 256 keys
-  const int fill = p.T == 4 ? 1024 : 4096;
+  const int fill = rows > 32 ? 1024 : 4096;
   long long want = items >= fill ? 1 : (fill + items - 1) / items;
   if (want > most) want = most;
   if (want < 1) want = 1;

@@ -19,6 +19,8 @@ struct QuantAttnArgs {
   int row_blocks, pieces, piece_keys;
   float scale_log2;                              // softmax scale times log2(e)
 };
+// Most tiles of 16 queries for which accumulators, queries and two groups of keys fit the 256 registers of two wavefronts a SIMD.
+static inline constexpr int quant_attn_tiles(int KQ, int W) { return W == 8 || (W == 4 && KQ == 4) ? 2 : 4; }
 // Queries of a wavefront in tiles of 16 (T), 32-dim steps of a key (KQ), dims of a value row a lane holds (W: 2, 4 or 8 of 32, 64 or 128).
 hipError_t quant_attn_launch_w2(const QuantAttnArgs& a, int T, int KQ, hipStream_t st);
 hipError_t quant_attn_launch_w4(const QuantAttnArgs& a, int T, int KQ, hipStream_t st);
