@@ -17,6 +17,7 @@ typedef __bf16 qa_bf16x2 __attribute__((ext_vector_type(2)));
 typedef float qa_floatx4 __attribute__((ext_vector_type(4)));
 typedef float qa_floatx8 __attribute__((ext_vector_type(8)));
 typedef unsigned qa_uintx4 __attribute__((ext_vector_type(4)));
+typedef unsigned qa_uintx2 __attribute__((ext_vector_type(2)));
 
 #define QA_RESCALE 8.0f        // growth of a row's maximum, in binades, that brings its sums to the new one
 #define QA_LN2 0.6931471805599453f
@@ -42,6 +43,13 @@ __device__ __forceinline__ float qa_sum4(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// ONCE: past the caches
+template <bool ONCE, typename V>
+__device__ __forceinline__ V qa_load(const unsigned char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+  else return *reinterpret_cast<const V*>(p);
+}
+
 // One group of 32 keys as it comes from memory.
 template <int KQ, int W>
 struct QaRaw {
@@ -65,8 +73,8 @@ __device__ __forceinline__ void qa_finish_row(float& m, float& l, float& in, con
   }
 }
 
-template <int T, int KQ, int W>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T == 1 && W < 8 ? (KQ < 4 ? 4 : 3) : 2)))
+template <int T, int KQ, int W, bool ONCE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(T == 1 ? (W < 8 && KQ < 4 ? 4 : 3) : 2)))
 void quant_attn_kernel(const QuantAttnArgs a) {
   constexpr int WAVES = 4, ROWS = 16 * T, KV = 16 * W, PITCH = KV + 4;
   __shared__ __attribute__((aligned(16))) float lds_o[WAVES][16][PITCH];
@@ -79,7 +87,8 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   const int len = min(max(a.lens[b], 0), a.own_max), row0 = rb * ROWS, row_last = min(row0 + ROWS, a.rows) - 1;
   // keys that the first and the last of these queries see
   const int sees_first = len - a.L + 1 + row0 / a.g, sees_last = len - a.L + 1 + row_last / a.g;
-  const int key0 = piece * a.piece_keys, key1 = min(key0 + a.piece_keys, sees_last);
+  // pieces of equal length, by the request's own number of keys: ragged lengths then make no empty ones (a multiple of the four wavefronts' groups)
+  const int piece_keys = ((len + a.pieces - 1) / a.pieces + 127) & ~127, key0 = piece * piece_keys, key1 = min(key0 + piece_keys, sees_last);
 
   qa_bf16x8 qf[T][KQ];
   int sees[T];
@@ -107,45 +116,46 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   }
   const unsigned vd = W * l16 < a.kv ? W * l16 : 0, kst = static_cast<unsigned>(a.k_st), vst = static_cast<unsigned>(a.v_st);
 
-  // a lane's rows of a group; in the last one of a piece those beyond the last key repeat it: nothing behind a length is read
-  unsigned koff[2], voff[8];
-  const auto aim = [&](int most) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) koff[i] = static_cast<unsigned>(min(16 * i + l16, most)) * kst;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) voff[e] = static_cast<unsigned>(min(16 * (e >> 2) + 4 * g + (e & 3), most)) * vst + vd;
-  };
-  aim(31);
-  const auto load = [&](int c, QaRaw<KQ, W>& x) __attribute__((always_inline)) {
-    const int k0 = c * 32;
-    if (k0 + 32 > key1) aim(key1 - 1 - k0);
-    const unsigned char* const kp = kb + static_cast<long long>(k0) * a.k_st;
-    const unsigned char* const vp = vb + static_cast<long long>(k0) * a.v_st;
+  const auto fetch = [&](const unsigned char* kp, const unsigned char* vp, auto&& krow, auto&& vrow, QaRaw<KQ, W>& x) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int s = 0; s < KQ; s += 2) {
         if (s + 1 < KQ) {
-          const uint4 u = *reinterpret_cast<const uint4*>(kp + (koff[i] + kd[s / 2]));
+          const qa_uintx4 u = qa_load<ONCE, qa_uintx4>(krow(kp, i) + kd[s / 2]);
           x.k[i][2 * s] = u.x; x.k[i][2 * s + 1] = u.y;
           x.k[i][(2 * s + 2) % (2 * KQ)] = u.z; x.k[i][(2 * s + 3) % (2 * KQ)] = u.w;
         } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(kp + (koff[i] + kd[s / 2]));
+          const qa_uintx2 u = qa_load<ONCE, qa_uintx2>(krow(kp, i) + kd[s / 2]);
           x.k[i][2 * s] = u.x; x.k[i][2 * s + 1] = u.y;
         }
       }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const unsigned char* const p = vp + voff[e];
+      const unsigned char* const p = vrow(vp, e);
       if constexpr (W == 8) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        const qa_uintx2 u = qa_load<ONCE, qa_uintx2>(p);
         x.v[e][0] = u.x; x.v[e][W > 4 ? 1 : 0] = u.y;
       } else if constexpr (W == 4) {
-        x.v[e][0] = *reinterpret_cast<const unsigned*>(p);
+        x.v[e][0] = qa_load<ONCE, unsigned>(p);
       } else {
-        x.v[e][0] = *reinterpret_cast<const unsigned short*>(p);
+        x.v[e][0] = qa_load<ONCE, unsigned short>(p);
       }
+    }
+  };
+  const unsigned klane = l16 * kst, vlane = 4 * g * vst + vd;
+  const auto load = [&](int c, QaRaw<KQ, W>& x) __attribute__((always_inline)) {
+    const int k0 = c * 32;
+    const unsigned char* const kp = kb + static_cast<long long>(k0) * a.k_st;
+    const unsigned char* const vp = vb + static_cast<long long>(k0) * a.v_st;
+    if (k0 + 32 <= key1) {
+      fetch(kp, vp, [&](const unsigned char* p, int i) __attribute__((always_inline)) { return p + 16 * i * a.k_st + klane; },
+            [&](const unsigned char* p, int e) __attribute__((always_inline)) { return p + (16 * (e >> 2) + (e & 3)) * a.v_st + vlane; }, x);
+    } else {      // rows beyond the last key repeat it: nothing behind a length is read
+      const int most = key1 - 1 - k0;
+      fetch(kp, vp, [&](const unsigned char* p, int i) __attribute__((always_inline)) { return p + static_cast<unsigned>(min(16 * i + l16, most)) * kst; },
+            [&](const unsigned char* p, int e) __attribute__((always_inline)) { return p + (static_cast<unsigned>(min(16 * (e >> 2) + 4 * g + (e & 3), most)) * vst + vd); }, x);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -309,15 +319,15 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   }
 }
 
-template <int T, int KQ, int W>
+template <int T, int KQ, int W, bool ONCE>
 static hipError_t quant_attn_launch(const QuantAttnArgs& a, hipStream_t st) {
   const int groups = (a.B * a.h_kv + 7) / 8 * 8;
-  hipLaunchKernelGGL((quant_attn_kernel<T, KQ, W>), dim3(static_cast<unsigned>(groups) * a.row_blocks * a.pieces), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((quant_attn_kernel<T, KQ, W, ONCE>), dim3(static_cast<unsigned>(groups) * a.row_blocks * a.pieces), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <int W>
-static hipError_t quant_attn_dispatch(const QuantAttnArgs& a, int T, int KQ, hipStream_t st) {
-#define QA_CASE(t, k) if constexpr (t <= quant_attn_tiles(k, W)) if (T == t && KQ == k) return quant_attn_launch<t, k, W>(a, st);
+static hipError_t quant_attn_dispatch(const QuantAttnArgs& a, int T, int KQ, bool once, hipStream_t st) {
+#define QA_CASE(t, k) if constexpr (t <= quant_attn_tiles(k, W)) if (T == t && KQ == k) return t == 1 && once ? quant_attn_launch<t, k, W, t == 1>(a, st) : quant_attn_launch<t, k, W, false>(a, st);
   QA_CASE(1, 1) QA_CASE(1, 2) QA_CASE(1, 3) QA_CASE(1, 4) QA_CASE(2, 1) QA_CASE(2, 2) QA_CASE(2, 3) QA_CASE(2, 4) QA_CASE(4, 1) QA_CASE(4, 2) QA_CASE(4, 3) QA_CASE(4, 4)
 #undef QA_CASE
   return hipErrorInvalidValue;

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void quant_attn_join_kernel(const QuantAttnArg
 }
 
 // Tiles of 16 queries a wavefront takes, and how many pieces the keys of a head are cut into.
-struct QuantPlan { int T, row_blocks, pieces, piece_keys, W; };
+struct QuantPlan { int T, row_blocks, pieces, W; };
 static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {
   QuantPlan p;
   const int rows = c->h / c->h_kv * L;
@@ -72,16 +72,11 @@ static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {
   p.T = rows <= 16 ? 1 : (rows <= 32 || quant_attn_tiles((c->kp_qk + 31) / 32, p.W) == 2 ? 2 : 4);
   p.row_blocks = (rows + 16 * p.T - 1) / (16 * p.T);
   const long long items = static_cast<long long>(c->B) * c->h_kv * p.row_blocks;
-  const int most = (c->own_max + 255) / 256;      // pieces of at least 256 keys
-  const int fill = rows > 32 ? 1024 : 4096;
+  const int most = (c->own_max + 511) / 512, fill = rows > 32 ? 1024 : 512;
   long long want = items >= fill ? 1 : (fill + items - 1) / items;
   if (want > most) want = most;
   if (want < 1) want = 1;
-  p.piece_keys = static_cast<int>((c->own_max + want - 1) / want);
-  p.piece_keys = (p.piece_keys + 127) / 128 * 128;
-  if (p.piece_keys < 128) p.piece_keys = 128;
-  p.pieces = (c->own_max + p.piece_keys - 1) / p.piece_keys;
-  if (p.pieces < 1) p.pieces = 1;
+  p.pieces = static_cast<int>(want);
   return p;
 }
 static size_t quant_part_bytes(const ecospa_quant_cache* c, const QuantPlan& p) {
@@ -118,11 +113,12 @@ extern "C" int ecospa_quant_cache_attn(ecospa_ctx* ctx, const ecospa_quant_cache
   a.B = c->B; a.L = L; a.h = c->h; a.h_kv = c->h_kv; a.g = c->h / c->h_kv; a.rows = a.g * L; a.kq = c->kp_qk; a.kv = c->kp_vo; a.own_max = c->own_max;
   a.block_log2 = 31 - __builtin_clz(static_cast<unsigned>(c->block));
   a.blocks = (c->cap + c->block - 1) / c->block;
-  a.row_blocks = p.row_blocks; a.pieces = p.pieces; a.piece_keys = p.piece_keys;
+  a.row_blocks = p.row_blocks; a.pieces = p.pieces;
   a.scale_log2 = c->scale * 1.4426950408889634f;
   if (static_cast<long long>(c->B * c->h_kv + 7) * p.row_blocks * p.pieces > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
   const int KQ = (c->kp_qk + 31) / 32;
-  const hipError_t e = p.W == 2 ? quant_attn_launch_w2(a, p.T, KQ, ctx->stream) : p.W == 4 ? quant_attn_launch_w4(a, p.T, KQ, ctx->stream) : quant_attn_launch_w8(a, p.T, KQ, ctx->stream);
+  const bool once = static_cast<long long>(c->B) * c->h_kv * c->own_max * (c->kp_qk + c->kp_vo) > 96ll << 20;
+  const hipError_t e = p.W == 2 ? quant_attn_launch_w2(a, p.T, KQ, once, ctx->stream) : p.W == 4 ? quant_attn_launch_w4(a, p.T, KQ, once, ctx->stream) : quant_attn_launch_w8(a, p.T, KQ, once, ctx->stream);
   if (e != hipSuccess) return hip_fail(ctx, e, "quant_attn_kernel");
   if (p.pieces > 1) {
     const long long rows = static_cast<long long>(c->B) * c->h_kv * a.rows;

@@ -1,4 +1,4 @@
 // Attention over caches of 8-bit floats, value rows of up to 64 dims.
 #include "quant_attn.h"
 
-hipError_t quant_attn_launch_w4(const QuantAttnArgs& a, int T, int KQ, hipStream_t st) { return quant_attn_dispatch<4>(a, T, KQ, st); }
+hipError_t quant_attn_launch_w4(const QuantAttnArgs& a, int T, int KQ, bool once, hipStream_t st) { return quant_attn_dispatch<4>(a, T, KQ, once, st); }
