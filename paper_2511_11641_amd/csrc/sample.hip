@@ -1,41 +1,47 @@
 // A token drawn for every row of logits by a given random number, after temperature, top-k, top-p and min-p.
 //
-// A token of logit x weighs 2^(t - e), t = x log2(e) / T, with e the whole number at or above the row's largest t; weights are held as whole numbers of
+// A token of logit x weighs 2^(t - e), t = x log2(e) / T, with e the whole number at or above the largest t; weights are held as whole numbers of
 // 2^-42, so that sums are exact in any order and results repeat.  All three restrictions keep a leading part of the tokens in order (larger logits
 // first, equal ones by index), so what is kept is everything up to one token, the border.  Nothing is sorted:
 //   scan    A workgroup takes a range of a row, once through memory: its largest logit, the weights relative to its own binade (a shift brings them to the
-//           row's later on), their sums over chunks of 512 tokens, and a histogram of counts and weights in bins of an eighth of a binade.
-//   draw    A workgroup a row: the ranges' histograms are added, the bin with the border is found, and the chunks that reach up to that bin are read again
-//           (they are in the last-level cache): weights above it are summed by chunk, the tokens in it go to a list in LDS, where the border is found digit by digit
-//           of (logit, index).  Then the chunk that the random number falls into, and the token in it.
+//           row's later on), and a histogram of weights (and counts) in bins of a sixteenth of a binade.
+//   draw    A workgroup a row: the ranges' histograms are added and the bin with the border is found; the row is read again (it is in the last-level cache), by
+//           comparisons alone, for the tokens of that bin, which go to a list in LDS; there the border is found digit by digit of (logit, index).  The histograms
+//           then say what every range keeps, hence the range that the random number falls into; only its weights are computed again.
 // Weights decide on whole tokens next to borders, so they are good to 2^-42: a table of 64 powers and four terms of the series in 64 bits, which run at the rate
-// of 32 bits here (some 25 instructions a token, at fp32 about as long as the memory takes).
+// of 32 bits here.
 #include "common.h"
+
+#include <type_traits>
 
 typedef unsigned long long smp_u64;
 
 #define SMP_BITS 42
-#define SMP_BINS (SMP_BITS * 8 + 16)     // an eighth of a binade each; the least weight, 1, is rounded from half a binade below 2^0
+#define SMP_BIN_LOG2 4                   // bins of a binade
+#define SMP_LEAST (64 * (SMP_BITS + 4))  // places, in 64ths of a binade below e: further down is as far down as nothing
+#define SMP_BINS ((SMP_LEAST >> (6 - SMP_BIN_LOG2)) + 4)
 #define SMP_CHUNK 512                    // tokens of a chunk: 8 a lane
-#define SMP_MAX_V (1 << 20)              // 42 bits of a weight and 20 of a vocabulary: sums below 2^62
+#define SMP_MAX_V (1 << 20)              // 42 bits of a weight and 20 of a vocabulary: sums below 2^63
 #define SMP_MAX_RANGES 512
 #define SMP_LIST 4096
+#define SMP_SHORT 256
 #define SMP_DRAW 1024
 
 struct SamplePart {
   double e;              // binade that the range's weights are relative to
+  smp_u64 total;         // their sum
   float top;             // largest logit, -inf: none
-  int at;                // its lowest token
+  int at;                // its lowest token (greedy rows alone)
   int bins;              // histogram bins in use
+  int pad;
 };
 struct SampleArgs {
   ecospa_sample_args q;
   SamplePart* part;      // [B][ranges]
   float* chunk_top;      // [B][chunks]
-  smp_u64* chunk_sum;    // [B][chunks], relative to their range
   smp_u64* bin_sum;      // [B][ranges][SMP_BINS]
   unsigned* bin_count;   // [B][ranges][SMP_BINS]
-  int range, ranges, chunks;      // tokens of a range (a multiple of SMP_CHUNK)
+  int range, range_log2, ranges, chunks;      // tokens of a range (a multiple of SMP_CHUNK)
 };
 
 constexpr double smp_power(int j) {      // 2^(j / 64)
@@ -47,37 +53,53 @@ constexpr double smp_power(int j) {      // 2^(j / 64)
 struct SamplePowers { double p[64]; };
 constexpr SamplePowers smp_powers() {
   SamplePowers t{};
-  for (int j = 0; j < 64; ++j) t.p[j] = smp_power(j);
+  for (int j = 0; j < 64; ++j) t.p[j] = smp_power(j) * (1ull << SMP_BITS);
   return t;
 }
 __device__ const SamplePowers SMP_POWERS = smp_powers();
 
-// The binade of a range whose largest logit is `top`, and the place of that logit, 64 (t - e).  (A temperature so small that a place has no fraction left: 0.)
+// Where a logit of a range lies, in 64ths of a binade relative to the range's e.  Ordinary: one fused step.  Where the largest is +inf (it alone, with its equals,
+// weighs then), or a temperature so small that places have no fraction left: by the distance to the largest, which is at 0.
+struct SampleScale {
+  double c64, off;
+  float top;
+  bool plain;
+};
 __device__ __forceinline__ double smp_binade(float top, double c64) {
   return fabsf(top) == INFINITY ? 0.0 : __builtin_ceil(static_cast<double>(top) * c64 * (1.0 / 64.0));
 }
-__device__ __forceinline__ double smp_base(float top, double c64, double e) {
-  return fabsf(top) == INFINITY || __builtin_fabs(e) > 1e13 ? 0.0 : __builtin_fma(static_cast<double>(top), c64, -64.0 * e);
+__device__ __forceinline__ SampleScale smp_scale(float top, double c64, double e) {
+  const bool plain = fabsf(top) < INFINITY && __builtin_fabs(e) < 1e12;
+  return {c64, plain ? -64.0 * e : 0.0, top, plain};
 }
-// 64 (t - e) of a logit of that range, from its distance to `top`, which 64 bits hold; what has no weight (NaN, -inf, a finite one beside +inf) is far below
-__device__ __forceinline__ double smp_place(float x, float top, double c64, double base) {
-  const double u = x == top ? base : __builtin_fma(static_cast<double>(x) - static_cast<double>(top), c64, base);
-  return __builtin_fmax(u, -64.0 * (SMP_BITS + 4));
+template <bool PLAIN>
+__device__ __forceinline__ double smp_place_as(float x, const SampleScale& s) {      // no weight (NaN, -inf): far below
+  if constexpr (PLAIN) return __builtin_fmax(__builtin_fma(static_cast<double>(x), s.c64, s.off), -1.0 * SMP_LEAST);
+  else return x == s.top ? 0.0 : __builtin_fmax((static_cast<double>(x) - static_cast<double>(s.top)) * s.c64, -1.0 * SMP_LEAST);
 }
-// its weight times 2^42, not rounded; k: the place in whole 64ths (<= 0 but for a rounding)
-__device__ __forceinline__ double smp_weight(double u, const double* powers, int& k) {
-  const double w = __builtin_rint(u), r = (u - w) * (0.69314718055994530942 / 64.0);
-  k = static_cast<int>(w);
-  double p = __builtin_fma(r, 1.0 / 24.0, 1.0 / 6.0);
-  p = __builtin_fma(p, r, 0.5);
-  p = __builtin_fma(p, r, 1.0);
-  p = __builtin_fma(p, r, 1.0);
-  return __builtin_ldexp(p * powers[k & 63], SMP_BITS + (k >> 6));
+__device__ __forceinline__ double smp_place(float x, const SampleScale& s) { return s.plain ? smp_place_as<true>(x, s) : smp_place_as<false>(x, s); }
+// The weight times 2^42 of a place u as two factors: a power of the table, moved by whole binades, and the series.  k: u in whole 64ths (the low bits of u + 1.5 2^52).
+struct SampleWeight {
+  double power, series;
+  int k;
+};
+__device__ __forceinline__ SampleWeight smp_weight(double u, const double* powers) {
+  constexpr double L = 0.69314718055994530942 / 64.0, M = 6755399441055744.0;
+  const double m = u + M, r = u - (m - M);
+  SampleWeight w;
+  w.k = static_cast<int>(__builtin_bit_cast(smp_u64, m));
+  double p = __builtin_fma(r, L * L * L * L / 24.0, L * L * L / 6.0);
+  p = __builtin_fma(p, r, L * L / 2.0);
+  p = __builtin_fma(p, r, L);
+  w.series = __builtin_fma(p, r, 1.0);
+  const smp_u64 t = __builtin_bit_cast(smp_u64, powers[w.k & 63]);
+  w.power = __builtin_bit_cast(double, t + (static_cast<smp_u64>(static_cast<unsigned>(w.k >> 6)) << 52));
+  return w;
 }
-__device__ __forceinline__ smp_u64 smp_whole(double w) {      // nearest whole number of w < 2^51: the low bits of 2^52 + w
-  return __builtin_bit_cast(smp_u64, w + 4503599627370496.0) & 0xfffffffffffffull;
+__device__ __forceinline__ smp_u64 smp_whole(const SampleWeight& w) {      // the nearest whole number: the low bits of 2^52 + the weight
+  return __builtin_bit_cast(smp_u64, __builtin_fma(w.series, w.power, 4503599627370496.0)) & 0xfffffffffffffull;
 }
-__device__ __forceinline__ int smp_bin(int k) { return min(max(-k, 0) >> 3, SMP_BINS - 1); }
+__device__ __forceinline__ int smp_bin(int k) { return max(-k, 0) >> (6 - SMP_BIN_LOG2); }
 // larger logits first: ascending numbers, -0 with +0 (NaN has no weight and is never asked for)
 __device__ __forceinline__ unsigned smp_rank(float x) {
   const unsigned b = __float_as_uint(x + 0.f);
@@ -147,16 +169,22 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
   __shared__ double powers[64];
   __shared__ float red_top[WAVES];
   __shared__ int red_at[WAVES], used;
+  __shared__ smp_u64 total;
   const ecospa_sample_args& q = a.q;
   const int b = blockIdx.y, v0 = blockIdx.x * a.range, n = min(a.range, q.V - v0), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const T* const row = static_cast<const T*>(q.logits) + b * q.ld + v0;
   float x[CH][8];
+  if (n == a.range) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c) smp_load(row + (c * WAVES + wave) * SMP_CHUNK + lane * 8, n - (c * WAVES + wave) * SMP_CHUNK - lane * 8, x[c]);
+    for (int c = 0; c < CH; ++c) smp_load(row + (c * WAVES + wave) * SMP_CHUNK + lane * 8, 8, x[c]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) smp_load(row + (c * WAVES + wave) * SMP_CHUNK + lane * 8, n - (c * WAVES + wave) * SMP_CHUNK - lane * 8, x[c]);
+  }
   const SampleRow r = smp_row(q, b);
-  const bool bins = !r.greedy && (r.by_k || r.by_p);
+  const bool bins = !r.greedy && (r.by_k || r.by_p || r.by_min);
   if (tid < 64) powers[tid] = SMP_POWERS.p[tid];
-  if (tid == 0) used = 0;
+  if (tid == 0) { used = 0; total = 0; }
   if (bins) {
     for (int i = tid; i < SMP_BINS; i += THREADS) { sum[i] = 0; count[i] = 0; }
   }
@@ -188,34 +216,38 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
     if (tid == 0) {
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) at = min(at, static_cast<unsigned>(red_at[w]));
-      *part = SamplePart{0.0, top, v0 + static_cast<int>(at), 0};
+      *part = SamplePart{0.0, 0, top, v0 + static_cast<int>(at), 0, 0};
     }
     return;
   }
-  const double e = smp_binade(top, r.c64), base = smp_base(top, r.c64, e);
-  int most = 0;
+  const double e = smp_binade(top, r.c64);
+  const SampleScale scale = smp_scale(top, r.c64, e);
+  int most = -1;
+  smp_u64 s = 0;
+  const auto weigh = [&](auto plain) __attribute__((always_inline)) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    smp_u64 s = 0;
+    for (int c = 0; c < CH; ++c) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int k;
-      const smp_u64 w = smp_whole(smp_weight(smp_place(x[c][i], top, r.c64, base), powers, k));
-      s += w;
-      if (bins && w != 0) {
-        const int bin = smp_bin(k);
-        atomicAdd(&sum[bin], w);
-        if (r.by_k) atomicAdd(&count[bin], 1u);
-        most = max(most, bin + 1);
+      for (int i = 0; i < 8; ++i) {
+        const SampleWeight wt = smp_weight(smp_place_as<decltype(plain)::value>(x[c][i], scale), powers);
+        const smp_u64 w = smp_whole(wt);
+        s += w;
+        if (bins && w != 0) {
+          const int bin = smp_bin(wt.k);
+          atomicAdd(&sum[bin], w);
+          if (r.by_k) atomicAdd(&count[bin], 1u);
+          most = max(most, bin);
+        }
       }
     }
-    s = smp_wave_sum(s);
-    const int chunk = c * WAVES + wave;
-    if (lane == 0 && chunk * SMP_CHUNK < n) a.chunk_sum[static_cast<long long>(b) * a.chunks + blockIdx.x * (a.range / SMP_CHUNK) + chunk] = s;
-  }
-  if (bins && most > 0) atomicMax(&used, most);
+  };
+  if (scale.plain) weigh(std::true_type{});
+  else weigh(std::false_type{});
+  s = smp_wave_sum(s);
+  if (lane == 0) atomicAdd(&total, s);
+  if (most >= 0) atomicMax(&used, most + 1);
   __syncthreads();
-  if (tid == 0) *part = SamplePart{e, top, 0, used};
+  if (tid == 0) *part = SamplePart{e, total, top, 0, used, 0};
   if (bins) {
     const long long at = (static_cast<long long>(b) * a.ranges + blockIdx.x) * SMP_BINS;
     for (int i = tid; i < used; i += THREADS) {
@@ -229,107 +261,132 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
 // draw
 // ---------------------------------------------------------------------------------------------
 struct SampleShared {
-  smp_u64 chunk[SMP_MAX_V / SMP_CHUNK];      // kept weight by chunk
-  smp_u64 list_key[SMP_LIST], list_w[SMP_LIST];
+  smp_u64 list_key[SMP_LIST], list_w[SMP_LIST];      // weights relative to their range
+  smp_u64 kept[SMP_MAX_RANGES];                       // kept weight by range, relative to it
   smp_u64 sum[SMP_BINS];
   unsigned count[SMP_BINS];
   smp_u64 digit_sum[256];
   unsigned digit_count[256];
-  double powers[64], base[SMP_MAX_RANGES];
-  float top[SMP_MAX_RANGES];
-  int shift[SMP_MAX_RANGES];                 // binades below the row's; 63: no weight
-  smp_u64 scan[SMP_DRAW / 64];
-  smp_u64 out[4];
-  int flag[4];
+  double powers[64];
+  SampleScale scale[SMP_MAX_RANGES];
+  int shift[SMP_MAX_RANGES], bins[SMP_MAX_RANGES];    // binades below the row's (63: no weight); histogram bins in use
+  float lo[SMP_MAX_RANGES], hi[SMP_MAX_RANGES];       // logits that can fall into the bin that is looked for
+  smp_u64 chunk[SMP_DRAW / 64], scan[SMP_DRAW / 64], scan_w[SMP_DRAW / 64], out[4];
   float red_f[SMP_DRAW / 64];
   double red_d[SMP_DRAW / 64];
   int listed;
 };
-__device__ __forceinline__ smp_u64 smp_inclusive(smp_u64 v) {      // over the lanes of a wavefront
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const smp_u64 u = __shfl_up(v, off, 64);
-    if ((threadIdx.x & 63) >= static_cast<unsigned>(off)) v += u;
+static_assert(sizeof(SampleShared) <= 120 * 1024, "LDS of a compute unit");
+static_assert(SMP_BINS <= SMP_DRAW, "a bin a thread");
+// running sums over the lanes of a wavefront, by lane permutations; ROWS: over every 16 lanes
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ smp_u64 smp_moved(smp_u64 v) {      // 0 where a lane has no source
+  const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROW_MASK, 0xF, true));
+  const unsigned hi = static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v >> 32), CTRL, ROW_MASK, 0xF, true));
+  return (static_cast<smp_u64>(hi) << 32) | lo;
+}
+template <bool ROWS = false>
+__device__ __forceinline__ smp_u64 smp_inclusive(smp_u64 v) {
+  v += smp_moved<0x111, 0xF>(v);
+  v += smp_moved<0x112, 0xF>(v);
+  v += smp_moved<0x114, 0xF>(v);
+  v += smp_moved<0x118, 0xF>(v);
+  if constexpr (!ROWS) {
+    v += smp_moved<0x142, 0xA>(v);      // lane 15 of a row to the next row: rows 1 and 3
+    v += smp_moved<0x143, 0xC>(v);      // lane 31 to rows 2 and 3
   }
   return v;
 }
-// One wavefront: the first of n bins where the running sum of v reaches `need` (the last bin that holds anything if none does), into out[0]; out[1], out[2]: sums of v
-// and of w over the bins in front of it; out[3]: 1 where `need` is reached.
-template <typename V, typename W>
-__device__ __forceinline__ void smp_find(int n, smp_u64 need, V&& v, W&& w, smp_u64* out) {
-  const int lane = threadIdx.x & 63, per = (n + 63) / 64;
-  smp_u64 mine = 0, other = 0;
-  int last = -1;
-  for (int i = 0; i < per; ++i) {
-    const int bin = lane * per + i;
-    if (bin >= n) break;
-    mine += v(bin);
-    other += w(bin);
-    if (v(bin) != 0) last = bin;
-  }
-  const smp_u64 upto = smp_inclusive(mine), upto_w = smp_inclusive(other);
-  const unsigned long long reached = __ballot(upto >= need), some = __ballot(last >= 0);
-  if (some == 0) {
-    if (lane == 0) { out[0] = 0; out[1] = out[2] = out[3] = 0; }
-    return;
-  }
-  const int from = reached ? __ffsll(reached) - 1 : 63 - __clzll(some);
-  if (lane == from) {
-    smp_u64 front = upto - mine, front_w = upto_w - other;
-    int bin = lane * per;
-    if (reached) {
-      for (; front + v(bin) < need; ++bin) { front += v(bin); front_w += w(bin); }
-    } else {
-      for (; bin < last; ++bin) { front += v(bin); front_w += w(bin); }
-    }
-    out[0] = static_cast<smp_u64>(bin);
-    out[1] = front;
-    out[2] = front_w;
-    out[3] = reached ? 1 : 0;
-  }
+__device__ __forceinline__ smp_u64 smp_lane(smp_u64 v, int l) {
+  const unsigned lo = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v), l)), hi = static_cast<unsigned>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), l));
+  return (static_cast<smp_u64>(hi) << 32) | lo;
 }
-
-template <typename T>
-struct SampleWalk {
-  const SampleArgs& a;
-  SampleShared& sh;
-  const T* row;
-  const float* chunk_top;
-  double c64;
-  int per_range;             // chunks
-  // place of a logit of range r relative to the row's binade
-  __device__ __forceinline__ double place(float x, int r) const {
-    return smp_place(x, sh.top[r], c64, sh.base[r]);
+// A value a wavefront, in LDS: the sum in front of this wavefront and that of all.  (A read a lane: sixteen reads of the whole wavefront would keep the LDS busy.)
+static_assert(SMP_DRAW == 16 * 64, "a row of lanes holds a value a wavefront");
+__device__ __forceinline__ smp_u64 smp_waves(const smp_u64* each, int wave, smp_u64& all) {
+  const smp_u64 own = each[threadIdx.x & 15], upto = smp_inclusive<true>(own);
+  all = smp_lane(upto, 15);
+  return smp_lane(upto - own, wave);
+}
+// The workgroup: the first of n <= SMP_DRAW bins where the running sum of v reaches `need(the sum of all)` (the last bin that holds anything if none does): its index,
+// the sums of v and of w over the bins in front of it, whether it is reached.  A bin a thread.  Every thread has left sh.scan, sh.scan_w and sh.out behind when it is called.
+struct SampleFound {
+  int bin;
+  smp_u64 front, front_w, need;
+  bool reached;
+};
+template <typename N, typename V, typename W>
+__device__ __forceinline__ SampleFound smp_find(SampleShared& sh, int n, N&& need_, V&& v, W&& w) {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));      // addresses are made here: kept over the phases of a draw they would not fit the registers
+  const int lane = tid & 63, wave = tid >> 6;
+  const smp_u64 own = tid < n ? v(tid) : 0, own_w = tid < n ? w(tid) : 0;
+  smp_u64 upto = own, upto_w = own_w;
+  if (wave * 64 < n) {
+    upto = smp_inclusive(own);
+    upto_w = smp_inclusive(own_w);
   }
-  // f(chunk, range, logits of the lane's eight tokens) for the wavefront's chunks that reach bin `least` or above it, AHEAD of them on their way together
-  template <int AHEAD, typename F, typename G>
-  __device__ __forceinline__ void chunks(int least, F&& f, G&& skipped) const {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (int c0 = wave; c0 < a.chunks; c0 += AHEAD * (SMP_DRAW / 64)) {
-      float x[AHEAD][8];
-      bool on[AHEAD];
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int c = c0 + i * (SMP_DRAW / 64);
-        on[i] = c < a.chunks;
-        if (on[i]) {
-          const int r = c / per_range, s = sh.shift[r];
-          const double u = place(chunk_top[c], r);
-          on[i] = s < 63 && smp_bin(static_cast<int>(__builtin_rint(u))) + 8 * s <= least;
-        }
-        on[i] = __builtin_amdgcn_readfirstlane(on[i]) != 0;
-        if (on[i]) smp_load(row + c * SMP_CHUNK + lane * 8, a.q.V - c * SMP_CHUNK - lane * 8, x[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < AHEAD; ++i) {
-        const int c = c0 + i * (SMP_DRAW / 64);
-        if (on[i]) f(c, c / per_range, x[i]);
-        else if (c < a.chunks) skipped(c);
-      }
+  if (lane == 63) { sh.scan[wave] = upto; sh.scan_w[wave] = upto_w; }
+  if (tid == 0) { sh.out[0] = 0; sh.out[1] = 0; sh.out[2] = 0; }
+  __syncthreads();
+  smp_u64 all, all_w;
+  const int w_ = __builtin_amdgcn_readfirstlane(wave);
+  upto += smp_waves(sh.scan, w_, all);
+  upto_w += smp_waves(sh.scan_w, w_, all_w);
+  SampleFound f;
+  f.need = need_(all);
+  f.reached = all >= f.need;
+  if (own != 0 && (f.reached ? upto >= f.need && upto - own < f.need : upto == all)) {
+    sh.out[0] = static_cast<smp_u64>(tid);
+    sh.out[1] = upto - own;
+    sh.out[2] = upto_w - own_w;
+  }
+  __syncthreads();
+  f.bin = static_cast<int>(sh.out[0]);
+  f.front = sh.out[1];
+  f.front_w = sh.out[2];
+  return f;
+}
+__device__ __forceinline__ smp_u64 smp_key(float x, int v) { return (static_cast<smp_u64>(smp_rank(x)) << 20) | static_cast<unsigned>(v); }
+__device__ __forceinline__ float smp_logit(smp_u64 key) {
+  const unsigned r = static_cast<unsigned>(key >> 20);
+  return __uint_as_float(r & 0x80000000u ? r : 0x7fffffffu - r);
+}
+__device__ __forceinline__ int smp_token(smp_u64 key) { return static_cast<int>(key & 0xfffffu); }
+
+// The border among the tokens of a short list (up to SMP_SHORT): every token's place in order is counted against all others, four lanes a token.
+__device__ __forceinline__ smp_u64 smp_border_short(SampleShared& sh, int n, int range_log2, smp_u64 need, bool counted, smp_u64& taken) {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int i = tid >> 2;
+  if (tid < n) sh.digit_sum[tid] = sh.list_w[tid] >> sh.shift[smp_token(sh.list_key[tid]) >> range_log2];
+  if (tid == 0) { sh.out[0] = ~0ull; sh.out[1] = 0; sh.out[2] = 0; }
+  __syncthreads();
+  if (i < n) {
+    const smp_u64 key = sh.list_key[i], w = sh.digit_sum[i];
+    smp_u64 front = 0;
+    unsigned front_n = 0;
+    for (int m = tid & 3; m < n; m += 4) {
+      const smp_u64 x = sh.digit_sum[m];
+      const bool in = sh.list_key[m] < key && x != 0;
+      front += in ? x : 0;
+      front_n += in ? 1u : 0u;
+    }
+    front += __shfl_xor(front, 1, 64);
+    front_n += __shfl_xor(front_n, 1, 64);
+    front += __shfl_xor(front, 2, 64);
+    front_n += __shfl_xor(front_n, 2, 64);
+    if ((tid & 3) == 0 && w != 0) {
+      atomicMax(&sh.out[2], front + w);
+      if (counted ? front_n + 1u == need : front < need && front + w >= need) { sh.out[0] = key; sh.out[1] = front + w; }
     }
   }
-};
-__device__ __forceinline__ smp_u64 smp_key(float x, int v) { return (static_cast<smp_u64>(smp_rank(x)) << 20) | static_cast<unsigned>(v); }
+  __syncthreads();
+  const smp_u64 key = sh.out[0];
+  taken = key == ~0ull ? sh.out[2] : sh.out[1];      // fewer than asked for: all of them
+  __syncthreads();
+  return key;
+}
 
 // The border among the tokens of one bin: the least key such that the tokens up to it hold `need` (tokens if `counted`, else weight).  each(f) calls
 // f(key, weight) for every token of the bin, over the threads of the workgroup.  -> the key; taken: weight up to it.
@@ -345,14 +402,14 @@ __device__ __forceinline__ smp_u64 smp_border(SampleShared& sh, smp_u64 need, bo
     lo = min(lo, static_cast<smp_u64>(__shfl_xor(lo, off, 64)));
     hi = max(hi, static_cast<smp_u64>(__shfl_xor(hi, off, 64)));
   }
-  if ((tid & 63) == 0) { atomicMin(&sh.out[0], lo); atomicMax(&sh.out[1], hi); }
+  if ((tid & 63) == 0 && lo <= hi) { atomicMin(&sh.out[0], lo); atomicMax(&sh.out[1], hi); }
   __syncthreads();
   lo = sh.out[0];
   hi = sh.out[1];
   __syncthreads();
   taken = 0;
   if (lo > hi) return 0;      // no token of any weight
-  int bits = 64 - __clzll((hi - lo) | 1ull), shift = max(bits - 8, 0);
+  int shift = max(64 - __clzll((hi - lo) | 1ull) - 8, 0);
   for (;;) {
     for (int i = tid; i < 256; i += SMP_DRAW) { sh.digit_sum[i] = 0; sh.digit_count[i] = 0; }
     __syncthreads();
@@ -363,15 +420,12 @@ __device__ __forceinline__ smp_u64 smp_border(SampleShared& sh, smp_u64 need, bo
       atomicAdd(&sh.digit_count[d], 1u);
     });
     __syncthreads();
-    if (tid < 64) {
-      const auto s = [&](int i) __attribute__((always_inline)) { return sh.digit_sum[i]; };
-      const auto c = [&](int i) __attribute__((always_inline)) { return static_cast<smp_u64>(sh.digit_count[i]); };
-      if (counted) smp_find(256, need, c, s, sh.out);
-      else smp_find(256, need, s, c, sh.out);
-    }
-    __syncthreads();
-    const int d = static_cast<int>(sh.out[0]);
-    const smp_u64 front = sh.out[1], front_other = sh.out[2], in_sum = sh.digit_sum[d], in_count = sh.digit_count[d];
+    const auto s = [&](int i) __attribute__((always_inline)) { return sh.digit_sum[i]; };
+    const auto c = [&](int i) __attribute__((always_inline)) { return static_cast<smp_u64>(sh.digit_count[i]); };
+    const auto n = [&](smp_u64) __attribute__((always_inline)) { return need; };
+    const SampleFound f = counted ? smp_find(sh, 256, n, c, s) : smp_find(sh, 256, n, s, c);
+    const int d = f.bin;
+    const smp_u64 front = f.front, front_other = f.front_w, in_sum = sh.digit_sum[d], in_count = sh.digit_count[d];
     __syncthreads();
     taken += counted ? front_other : front;
     need -= min(front, need);
@@ -390,13 +444,15 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
   extern __shared__ __attribute__((aligned(16))) char lds_sample[];
   SampleShared& sh = *reinterpret_cast<SampleShared*>(lds_sample);
   const ecospa_sample_args& q = a.q;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr int WAVES = SMP_DRAW / 64;
   const SampleRow r = smp_row(q, b);
   const SamplePart* const part = a.part + static_cast<long long>(b) * a.ranges;
   if (tid < 64) sh.powers[tid] = SMP_POWERS.p[tid];
+  const float* const chunk_top = a.chunk_top + static_cast<long long>(b) * a.chunks;
+  const float early_top = chunk_top[min(wave + lane * WAVES, a.chunks - 1)];      // the chunks that `walk` looks at first
   // the row's largest logit and binade
-  SamplePart mine{0.0, -INFINITY, 0, 0};
+  SamplePart mine{0.0, 0, -INFINITY, 0, 0, 0};
   if (tid < a.ranges) mine = part[tid];
   const float own_top = wave_max(mine.top);
   double e = mine.top == -INFINITY ? -__builtin_inf() : mine.e;
@@ -431,73 +487,140 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
     const double below = e - mine.e;
     const bool none = mine.top == -INFINITY || (infinite && mine.top != INFINITY) || below > SMP_BITS + 1;
     sh.shift[tid] = none ? 63 : static_cast<int>(below);
-    sh.top[tid] = mine.top;
-    sh.base[tid] = smp_base(mine.top, r.c64, mine.e);
+    sh.bins[tid] = none ? 0 : mine.bins;
+    sh.kept[tid] = none ? 0 : mine.total;
+    sh.scale[tid] = smp_scale(mine.top, r.c64, mine.e);
   }
   __syncthreads();
   const T* const row = static_cast<const T*>(q.logits) + b * q.ld;
-  const SampleWalk<T> walk{a, sh, row, a.chunk_top + static_cast<long long>(b) * a.chunks, r.c64, a.range / SMP_CHUNK};
-  // least place (64ths, relative to the row's binade) that min-p leaves
-  const double least_place = r.by_min ? smp_base(top, r.c64, e) + 64.0 * log2(static_cast<double>(r.min_p)) : -1e30;
-
-  int border_bin = SMP_BINS;      // tokens of lower bins are kept whole
-  smp_u64 border = 0;             // and of this bin those with keys up to this
-  if (r.by_k || r.by_p) {
+  const smp_u64* const bin_sums = a.bin_sum + static_cast<long long>(b) * a.ranges * SMP_BINS;
+  const unsigned* const bin_counts = a.bin_count + static_cast<long long>(b) * a.ranges * SMP_BINS;
+  const int per_log2 = a.range_log2 - 9;      // chunks of a range
+  const bool bounded = r.by_k || r.by_p || r.by_min;
+  // least place (relative to the row's binade) that min-p leaves, and its bin
+  const double least_place = r.by_min ? smp_place(top, smp_scale(top, r.c64, e)) + 64.0 * log2(static_cast<double>(r.min_p)) : -1e30;
+  const int least_bin = r.by_min ? smp_bin(static_cast<int>(__builtin_rint(__builtin_fmax(least_place, -1.0 * SMP_LEAST)))) : SMP_BINS;
+  if (bounded) {      // the row's histogram, eight ranges on their way together
     for (int i = tid; i < SMP_BINS; i += SMP_DRAW) {
       smp_u64 s = 0;
       unsigned c = 0;
-      for (int g = 0; g < a.ranges; ++g) {
-        const int by = sh.shift[g], from = i - 8 * by;
-        if (by >= 63 || from < 0 || from >= part[g].bins) continue;
-        const long long at = (static_cast<long long>(b) * a.ranges + g) * SMP_BINS + from;
-        s += a.bin_sum[at] >> by;
-        if (r.by_k) c += a.bin_count[at];
+      for (int g0 = 0; g0 < a.ranges; g0 += 8) {
+        smp_u64 x[8];
+        unsigned y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int g = min(g0 + u, a.ranges - 1), from = i - (sh.shift[g] << SMP_BIN_LOG2);
+          const bool in = g0 + u < a.ranges && from >= 0 && from < sh.bins[g];
+          const int at = g * SMP_BINS + max(from, 0);      // read in any case: loads under a condition are waited for one by one
+          x[u] = bin_sums[at] >> sh.shift[g];
+          y[u] = r.by_k ? bin_counts[at] : 0;
+          x[u] = in ? x[u] : 0;
+          y[u] = in ? y[u] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { s += x[u]; c += y[u]; }
       }
       sh.sum[i] = s;
       sh.count[i] = c;
     }
-    __syncthreads();
   }
   const auto bin_sum = [&](int i) __attribute__((always_inline)) { return sh.sum[i]; };
   const auto bin_count = [&](int i) __attribute__((always_inline)) { return static_cast<smp_u64>(sh.count[i]); };
-  // weights above `bin` by chunk (where `sums`), and the tokens in it to the list
-  const auto gather = [&](int bin, bool sums) __attribute__((always_inline)) {
+  // f(chunk, logits of the lane's eight tokens) for the wavefront's chunks that reach the bin that is looked for, AHEAD of them on their way together
+  const auto walk = [&](auto ahead_, auto&& f) __attribute__((always_inline)) {
+    constexpr int AHEAD = decltype(ahead_)::value;
+    for (int c1 = wave; c1 < a.chunks; c1 += 64 * WAVES) {
+      const int own = min(c1 + lane * WAVES, a.chunks - 1);      // a lane knows one chunk
+      const float own_most = c1 == wave ? early_top : chunk_top[own];
+      unsigned long long left = __ballot(c1 + lane * WAVES < a.chunks && own_most >= sh.lo[own >> per_log2]);
+      while (left) {
+        float x[AHEAD][8];
+        int c[AHEAD];
+        bool on[AHEAD], whole = true;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          on[i] = left != 0;
+          c[i] = on[i] ? c1 + __builtin_ctzll(left) * WAVES : c[0];      // none left: read again, to no use (a load under a condition is waited for by itself)
+          left &= left - 1;
+          whole = whole && (c[i] + 1) * SMP_CHUNK <= q.V;
+        }
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) smp_load(row + c[i] * SMP_CHUNK + lane * 8, 8, x[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) smp_load(row + c[i] * SMP_CHUNK + lane * 8, q.V - c[i] * SMP_CHUNK - lane * 8, x[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (on[i]) f(c[i], x[i]);
+      }
+    }
+  };
+  // the tokens of `bin` to the list: those whose logit can be in it first, then what they weigh
+  const auto gather = [&](int bin) __attribute__((always_inline)) {
     if (tid == 0) sh.listed = 0;
+    if (tid < a.ranges) {
+      const SampleScale& s = sh.scale[tid];
+      const int by = sh.shift[tid], width = 1 << (6 - SMP_BIN_LOG2);
+      float lo = INFINITY, hi = -INFINITY;
+      if (by < 63) {
+        lo = -INFINITY;
+        hi = INFINITY;
+        if (s.plain && s.c64 > 0.0) {      // places of the bin, and a little on both sides
+          const double u1 = 64.0 * by - width * bin, xl = (u1 - width - s.off) / s.c64, xh = (u1 + 1.0 - s.off) / s.c64;
+          lo = static_cast<float>(xl - (__builtin_fabs(xl) * 1e-6 + 1e-36));
+          hi = bin == 0 ? INFINITY : static_cast<float>(xh + (__builtin_fabs(xh) * 1e-6 + 1e-36));
+        }
+      }
+      sh.lo[tid] = lo;
+      sh.hi[tid] = hi;
+    }
     __syncthreads();
-    walk.template chunks<2>(bin, [&](int c, int g, const float (&x)[8]) __attribute__((always_inline)) {
-      const int by = sh.shift[g];
-      smp_u64 s = 0;
+    walk(std::integral_constant<int, sizeof(T) == 2 ? 4 : 2>{}, [&](int c, const float (&x)[8]) __attribute__((always_inline)) {
+      const float lo = sh.lo[c >> per_log2], hi = sh.hi[c >> per_log2];
+      const int v = c * SMP_CHUNK + lane * 8;
+      // few of them are: a bit each, then one token a lane and turn
+      float y[8];
+      unsigned bits = 0u;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const double u = walk.place(x[i], g);
-        const int k = static_cast<int>(__builtin_rint(u)), at = smp_bin(k) + 8 * by;
-        if (at > bin) continue;
-        int k2;
-        const smp_u64 w = smp_whole(smp_weight(u, sh.powers, k2)) >> by;
-        if (w == 0) continue;
-        if (at < bin) {
-          if (u - 64.0 * by >= least_place) s += w;
-        } else {
-          const int slot = atomicAdd(&sh.listed, 1);
-          if (slot < SMP_LIST) { sh.list_key[slot] = smp_key(x[i], c * SMP_CHUNK + lane * 8 + i); sh.list_w[slot] = w; }
-        }
-        __builtin_amdgcn_sched_barrier(0);      // one token behind the other: eight chains at once need more registers than there are
+        y[i] = x[i];
+        asm volatile("" : "+v"(y[i]));      // a register: chosen among by selects, not through memory
+        bits |= y[i] >= lo && y[i] <= hi ? 1u << i : 0u;
       }
-      if (sums) {
-        s = smp_wave_sum(s);
-        if (lane == 0) sh.chunk[c] = s;
+#pragma unroll 1
+      while (bits) {
+        const int i = __builtin_ctz(bits);
+        float yi = y[0];
+#pragma unroll
+        for (int m = 1; m < 8; ++m) yi = i == m ? y[m] : yi;
+        const int slot = atomicAdd(&sh.listed, 1);
+        if (slot < SMP_LIST) sh.list_key[slot] = smp_key(yi, v + i);
+        bits &= bits - 1;
       }
-    }, [&](int c) __attribute__((always_inline)) { if (sums && lane == 0) sh.chunk[c] = 0; });
+    });
+    __syncthreads();
+    for (int i = tid; i < min(sh.listed, SMP_LIST); i += SMP_DRAW) {
+      const smp_u64 key = sh.list_key[i];
+      const int g = smp_token(key) >> a.range_log2, by = sh.shift[g];
+      const SampleWeight w = smp_weight(smp_place(smp_logit(key), sh.scale[g]), sh.powers);
+      sh.list_w[i] = smp_bin(w.k) + (by << SMP_BIN_LOG2) == bin ? smp_whole(w) : 0;
+    }
     __syncthreads();
   };
-  // every token of `bin`, from the list or, where it did not hold them, from the row
+  // f(key, weight relative to its range, its shift) for every token of `bin`, from the list or, where it did not hold them, from the row
   const auto each_of = [&](int bin, auto&& f) __attribute__((always_inline)) {
     const int n = sh.listed;
     if (n <= SMP_LIST) {
-      for (int i = tid; i < n; i += SMP_DRAW) f(sh.list_key[i], sh.list_w[i]);
+      for (int i = tid; i < n; i += SMP_DRAW) {
+        const smp_u64 key = sh.list_key[i], w = sh.list_w[i];
+        const int by = sh.shift[smp_token(key) >> a.range_log2];
+        if (w >> by) f(key, w, by);
+      }
     } else {
-      walk.template chunks<1>(bin, [&](int c, int g, const float (&x)[8]) __attribute__((always_inline)) {
-        const int by = sh.shift[g];
+      walk(std::integral_constant<int, 1>{}, [&](int c, const float (&x)[8]) __attribute__((always_inline)) {
+        const int g = c >> per_log2, by = sh.shift[g];
         float y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = x[i];
@@ -506,138 +629,137 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
           const float xi = y[0];
 #pragma unroll
           for (int m = 0; m < 7; ++m) y[m] = y[m + 1];
-          int k;
-          const smp_u64 w = smp_whole(smp_weight(walk.place(xi, g), sh.powers, k)) >> by;
-          if (w != 0 && smp_bin(k) + 8 * by == bin) f(smp_key(xi, c * SMP_CHUNK + lane * 8 + i), w);
+          if (!(xi >= sh.lo[g] && xi <= sh.hi[g])) continue;
+          const SampleWeight wt = smp_weight(smp_place(xi, sh.scale[g]), sh.powers);
+          const smp_u64 w = smp_whole(wt);
+          if ((w >> by) != 0 && smp_bin(wt.k) + (by << SMP_BIN_LOG2) == bin) f(smp_key(xi, c * SMP_CHUNK + lane * 8 + i), w, by);
         }
-      }, [](int) __attribute__((always_inline)) {});
+      });
     }
   };
-  // by the number of tokens first: what is kept then is what top-p is a part of
+  int border_bin = SMP_BINS;      // tokens of lower bins are kept whole
+  smp_u64 border = ~0ull;         // and of this bin those with keys up to this
+  // by the number of tokens first: what is kept then is what top-p is a part of; min-p last
   smp_u64 total = 0;
   bool bordered = false;
-  int phase = r.by_k ? 0 : (r.by_p ? 1 : (r.by_min ? 2 : 3));      // tokens, weight, min-p alone, nothing more
+  int phase = r.by_k ? 0 : (r.by_p ? 1 : (r.by_min ? 2 : 3));
+  __syncthreads();
 #pragma unroll 1
   while (phase < 3) {
-    int bin = SMP_BINS;
-    smp_u64 front = 0, front_sum = 0;
+    int bin = least_bin;
+    smp_u64 front = 0, front_sum = 0, need = 0;
     bool reached = true;
-    smp_u64 need = static_cast<smp_u64>(r.k);
-    if (phase == 1) {
-      if (!bordered) {
-        if (tid < 64) {
-          smp_u64 s = 0;
-          for (int i = lane; i < SMP_BINS; i += 64) s += sh.sum[i];
-          s = smp_inclusive(s);
-          if (lane == 63) sh.out[0] = s;
-        }
-        __syncthreads();
-        total = sh.out[0];
-        __syncthreads();
-      }
-      // the least whole number of 2^-42 at or above top_p times the total
-      const smp_u64 p = r.p > 0.f ? static_cast<smp_u64>(static_cast<double>(r.p) * 4294967296.0) : 0ull;
-      const unsigned __int128 prod = static_cast<unsigned __int128>(total) * p;
-      need = max(static_cast<smp_u64>(prod >> 32) + (static_cast<unsigned>(static_cast<smp_u64>(prod)) != 0u ? 1 : 0), 1ull);
-    }
     if (phase < 2) {
-      if (tid < 64) {
-        if (phase == 0) smp_find(SMP_BINS, need, bin_count, bin_sum, sh.out);
-        else smp_find(SMP_BINS, need, bin_sum, bin_count, sh.out);
-      }
+      const smp_u64 k = static_cast<smp_u64>(r.k), p = r.p > 0.f ? static_cast<smp_u64>(static_cast<double>(r.p) * 4294967296.0) : 0ull;
+      const auto of_all = [&](smp_u64 all) __attribute__((always_inline)) {      // the least whole number of 2^-42 at or above top_p times the total
+        const unsigned __int128 prod = static_cast<unsigned __int128>(bordered ? total : all) * p;
+        return max(static_cast<smp_u64>(prod >> 32) + (static_cast<unsigned>(static_cast<smp_u64>(prod)) != 0u ? 1 : 0), 1ull);
+      };
+      const SampleFound f = phase == 0 ? smp_find(sh, SMP_BINS, [&](smp_u64) __attribute__((always_inline)) { return k; }, bin_count, bin_sum)
+                                       : smp_find(sh, SMP_BINS, of_all, bin_sum, bin_count);
+      bin = f.bin;
+      front = f.front;
+      need = f.need;
+      front_sum = phase == 0 ? f.front_w : front;
+      reached = f.reached;
       __syncthreads();
-      bin = static_cast<int>(sh.out[0]);
-      front = sh.out[1];
-      front_sum = phase == 0 ? sh.out[2] : front;
-      reached = sh.out[3] != 0;
-      __syncthreads();
+    } else if (border_bin <= least_bin) {      // min-p cuts behind the border or in its bin, whose list is there
+      break;
     }
+    const int next = phase == 0 && r.by_p ? 1 : (phase < 2 && r.by_min ? 2 : 3);
     if (phase == 0 && !reached) {      // fewer tokens than k weigh anything
-      phase = r.by_p ? 1 : (r.by_min ? 2 : 3);
+      phase = next;
       continue;
     }
-    gather(bin, phase != 0 || !r.by_p);
-    if (phase == 2) break;
-    smp_u64 taken;
-    border = smp_border(sh, max(need - min(front, need), 1ull), phase == 0, [&](auto&& f) __attribute__((always_inline)) { each_of(bin, f); }, taken);
+    if (next == 2 && bin > least_bin) {      // min-p cuts in front of it: where exactly it lies doesn't matter
+      border_bin = bin;
+      phase = next;
+      continue;
+    }
+    gather(bin);
+    border = ~0ull;
+    if (phase < 2) {
+      smp_u64 taken;
+      const smp_u64 rest = max(need - min(front, need), 1ull);
+      if (sh.listed <= SMP_SHORT)
+        border = smp_border_short(sh, sh.listed, a.range_log2, rest, phase == 0, taken);
+      else
+        border = smp_border(sh, rest, phase == 0,
+                          [&](auto&& f) __attribute__((always_inline)) { each_of(bin, [&](smp_u64 key, smp_u64 w, int by) __attribute__((always_inline)) { f(key, w >> by); }); }, taken);
+      total = front_sum + taken;
+      bordered = true;
+    }
     border_bin = bin;
-    bordered = true;
-    total = front_sum + taken;
-    phase = phase == 0 && r.by_p ? 1 : 3;
+    phase = next;
   }
-  if (bordered) {
-    // the kept tokens of the border's bin join their chunks' sums
-    each_of(border_bin, [&](smp_u64 key, smp_u64 w) __attribute__((always_inline)) {
-      if (key > border) return;
-      const int v = static_cast<int>(key & 0xfffffu), g = v / a.range;
-      if (r.by_min && walk.place(load_f32<T>(row + v), g) - 64.0 * sh.shift[g] < least_place) return;
-      atomicAdd(&sh.chunk[v / SMP_CHUNK], w);
+  const bool cut = border_bin < SMP_BINS;
+  const auto kept_there = [&](smp_u64 key, double place, int by) __attribute__((always_inline)) { return key <= border && place - 64.0 * by >= least_place; };
+  if (cut) {
+    // what every range keeps: its bins above the border's, and the border's tokens
+    for (int g = wave; g < a.ranges; g += WAVES) {
+      const int end = min(border_bin - (sh.shift[g] << SMP_BIN_LOG2), sh.bins[g]);
+      smp_u64 s = 0;
+      for (int i = lane; i < end; i += 64) s += bin_sums[g * SMP_BINS + i];
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, 64);
+      if (lane == 0) sh.kept[g] = s;
+    }
+    __syncthreads();
+    each_of(border_bin, [&](smp_u64 key, smp_u64 w, int by) __attribute__((always_inline)) {
+      const int g = smp_token(key) >> a.range_log2;
+      if (kept_there(key, smp_place(smp_logit(key), sh.scale[g]), by)) atomicAdd(&sh.kept[g], w);
     });
     __syncthreads();
   }
-  const bool whole = !bordered && !r.by_min;
-  if (whole) {
-    for (int c = tid; c < a.chunks; c += SMP_DRAW) {
-      const int by = sh.shift[c / walk.per_range];
-      sh.chunk[c] = by >= 63 ? 0 : a.chunk_sum[static_cast<long long>(b) * a.chunks + c] >> by;
-    }
-    __syncthreads();
-  }
 
-  // the chunk that the random number falls into
-  constexpr int PER = SMP_MAX_V / SMP_CHUNK / SMP_DRAW;
-  smp_u64 own[PER], all = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    own[i] = tid * PER + i < a.chunks ? sh.chunk[tid * PER + i] : 0;
-    all += own[i];
-  }
-  const smp_u64 upto = smp_inclusive(all);
+  // the range that the random number falls into
+  const smp_u64 own = tid < a.ranges && sh.shift[tid] < 63 ? sh.kept[tid] >> sh.shift[tid] : 0, upto = smp_inclusive(own);
   if (lane == 63) sh.scan[wave] = upto;
   __syncthreads();
-  smp_u64 front = 0;
-  total = 0;
-  for (int w = 0; w < WAVES; ++w) {
-    front += w < wave ? sh.scan[w] : 0;
-    total += sh.scan[w];
-  }
-  front += upto - all;
+  const smp_u64 front = smp_waves(sh.scan, wave, total) + upto - own;
   const float uf = q.u[b];
   const smp_u64 u = uf > 0.f ? (uf < 1.f ? static_cast<smp_u64>(static_cast<double>(uf) * 4294967296.0) : 4294967295ull) : 0ull;
   smp_u64 target = static_cast<smp_u64>((static_cast<unsigned __int128>(total) * u) >> 32);
-  if (!(uf < 1.f) && uf == uf) target = total - 1;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (target >= front && target < front + own[i]) {
-      sh.out[0] = static_cast<smp_u64>(tid * PER + i);
-      sh.out[1] = target - front;
-    }
-    front += own[i];
+  if (uf >= 1.f) target = total - 1;
+  if (target >= front && target < front + own) {
+    sh.out[0] = static_cast<smp_u64>(tid);
+    sh.out[1] = (target - front) << sh.shift[tid];      // relative to the range from here on
   }
   __syncthreads();
-  if (tid >= 64) return;
-  // the token
-  const int c = static_cast<int>(sh.out[0]), g = c / walk.per_range, by = sh.shift[g];
-  const smp_u64 into = whole ? sh.out[1] << by : sh.out[1];      // unrestricted sums are those of the range's own binade
-  float x[8];
-  smp_load(row + c * SMP_CHUNK + lane * 8, q.V - c * SMP_CHUNK - lane * 8, x);
-  smp_u64 w[8], s = 0;
+  const int g = static_cast<int>(sh.out[0]), by = sh.shift[g], n_chunks = 1 << per_log2, c = (g << per_log2) + wave;
+  smp_u64 into = sh.out[1], w[8], s = 0;
   double exact[8];
+  if (wave < n_chunks) {      // a wavefront a chunk
+    float x[8];
+    smp_load(row + c * SMP_CHUNK + lane * 8, q.V - c * SMP_CHUNK - lane * 8, x);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    int k;
-    const double p = walk.place(x[i], g);
-    exact[i] = smp_weight(p, sh.powers, k);
-    w[i] = smp_whole(exact[i]) >> (whole ? 0 : by);
-    const int at = smp_bin(k) + 8 * by;
-    const bool kept = whole || ((at < border_bin || (at == border_bin && smp_key(x[i], c * SMP_CHUNK + lane * 8 + i) <= border)) && p - 64.0 * by >= least_place);
-    w[i] = kept ? w[i] : 0;
-    s += w[i];
+    for (int i = 0; i < 8; ++i) {
+      const double p = smp_place(x[i], sh.scale[g]);
+      const SampleWeight wt = smp_weight(p, sh.powers);
+      const int at = smp_bin(wt.k) + (by << SMP_BIN_LOG2);
+      // a token of the border's bin that weighs nothing in the row's binade is not kept: it was not counted
+      const bool kept = !cut || at < border_bin || (at == border_bin && (smp_whole(wt) >> by) != 0 && kept_there(smp_key(x[i], c * SMP_CHUNK + lane * 8 + i), p, by));
+      exact[i] = wt.series * wt.power;
+      w[i] = kept ? smp_whole(wt) : 0;
+      s += w[i];
+    }
+    const smp_u64 all = smp_wave_sum(s);
+    if (lane == 0) sh.chunk[wave] = all;
   }
-  smp_u64 before = smp_inclusive(s) - s;
-  const unsigned long long have = __ballot(s != 0 && before <= into);      // the last lane that starts at or in front of the target
+  __syncthreads();
+  if (wave >= n_chunks) return;
+  smp_u64 before = 0;
+  int last = 0;      // the last chunk that starts at or in front of the target and holds anything
+  for (int i = 0; i < n_chunks; ++i) {
+    if (sh.chunk[i] != 0 && before <= into) last = i;
+    before += sh.chunk[i];
+  }
+  if (wave != last) return;
+  for (int i = 0; i < wave; ++i) into -= sh.chunk[i];
+  before = smp_inclusive(s) - s;
+  const unsigned long long have = __ballot(s != 0 && before <= into);      // the last lane, likewise
   if (lane != 63 - __clzll(have)) return;
-  int at = -1;
+  int at = 0;
   double weight = 0.0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -652,23 +774,22 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
 // entry points
 // ---------------------------------------------------------------------------------------------
 // Ranges of 8192 tokens; of 2048 while there are few of them.
-struct SamplePlan { int threads, range, ranges, chunks; };
+struct SamplePlan { int threads, range_log2, ranges, chunks; };
 static SamplePlan sample_plan(int B, int V) {
   SamplePlan p;
   const bool few = static_cast<long long>(B) * V <= 1 << 21;
   p.threads = few ? 256 : 512;
-  p.range = few ? 2048 : 8192;
-  p.ranges = (V + p.range - 1) / p.range;
+  p.range_log2 = few ? 11 : 13;
+  p.ranges = (V + (1 << p.range_log2) - 1) >> p.range_log2;
   p.chunks = (V + SMP_CHUNK - 1) / SMP_CHUNK;
   return p;
 }
 static void sample_carve(SampleArgs& a, const SamplePlan& p, WsCarver& ws, int B) {
-  const size_t n = static_cast<size_t>(B) * p.ranges, c = static_cast<size_t>(B) * p.chunks;
+  const size_t n = static_cast<size_t>(B) * p.ranges;
   a.part = static_cast<SamplePart*>(ws.take(n * sizeof(SamplePart)));
   a.bin_sum = static_cast<smp_u64*>(ws.take(n * SMP_BINS * sizeof(smp_u64)));
   a.bin_count = static_cast<unsigned*>(ws.take(n * SMP_BINS * sizeof(unsigned)));
-  a.chunk_sum = static_cast<smp_u64*>(ws.take(c * sizeof(smp_u64)));
-  a.chunk_top = static_cast<float*>(ws.take(c * sizeof(float)));
+  a.chunk_top = static_cast<float*>(ws.take(static_cast<size_t>(B) * p.chunks * sizeof(float)));
 }
 extern "C" size_t ecospa_sample_workspace_bytes(int B, int V) {
   if (B < 1 || V < 1 || B > 65535 || V > SMP_MAX_V) return 0;
@@ -691,7 +812,6 @@ static hipError_t sample_launch(const SampleArgs& a, const SamplePlan& p, hipStr
   hipLaunchKernelGGL(kern, dim3(a.q.B), dim3(SMP_DRAW), sizeof(SampleShared), st, a);
   return hipGetLastError();
 }
-static_assert(sizeof(SampleShared) <= 120 * 1024, "LDS of a compute unit");
 template __global__ void sample_draw_kernel<float>(const SampleArgs);
 template __global__ void sample_draw_kernel<bf16_t>(const SampleArgs);
 
@@ -707,7 +827,7 @@ extern "C" int ecospa_sample(ecospa_ctx* ctx, const ecospa_sample_args* q) {
   memset(&a, 0, sizeof(a));
   a.q = *q;
   const SamplePlan p = sample_plan(q->B, q->V);
-  a.range = p.range; a.ranges = p.ranges; a.chunks = p.chunks;
+  a.range = 1 << p.range_log2; a.range_log2 = p.range_log2; a.ranges = p.ranges; a.chunks = p.chunks;
   WsCarver ws(ctx->ws, ctx->ws_bytes);
   sample_carve(a, p, ws, q->B);
   if (!ws.ok()) return ECOSPA_ERR_WORKSPACE;
