@@ -9,7 +9,9 @@
 //           comparisons alone, for the tokens of that bin, which go to a list in LDS; there the border is found digit by digit of (logit, index).  The histograms
 //           then say what every range keeps, hence the range that the random number falls into; only its weights are computed again.
 // Weights decide on whole tokens next to borders, so they are good to 2^-42: a table of 64 powers and four terms of the series in 64 bits, which run at the rate
-// of 32 bits here.
+// of 32 bits here.  256 rows of 131072 fp32 logits with top-p and min-p: scan 53 us, bound by some 38 vector instructions a token (134 MB alone would be 21); draw 39 us,
+// where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps (20 us for one bf16 row of 32000 with top-k and top-p; scan 6.5).  Ranges of eight
+// tokens a lane times four wavefronts: registers for 32 logits a lane leave 4 wavefronts a SIMD, and that beats 16 (54 us) and 8 of a workgroup of 1024 (81).
 #include "common.h"
 
 #include <type_traits>
@@ -25,6 +27,7 @@ typedef unsigned long long smp_u64;
 #define SMP_MAX_RANGES 512
 #define SMP_LIST 4096
 #define SMP_SHORT 256
+#define SMP_SCAN 256
 #define SMP_DRAW 1024
 
 struct SamplePart {
@@ -50,10 +53,10 @@ constexpr double smp_power(int j) {      // 2^(j / 64)
   for (int i = 1; i < 24; ++i) { t *= x / i; s += t; }
   return s;
 }
-struct SamplePowers { double p[64]; };
-constexpr SamplePowers smp_powers() {
+struct SamplePowers { smp_u64 p[64]; };
+constexpr SamplePowers smp_powers() {      // bits of 2^(j / 64 + 42), less j << 14 in the upper word: k << 14 brings it back for k's low bits, and whole binades with it
   SamplePowers t{};
-  for (int j = 0; j < 64; ++j) t.p[j] = smp_power(j) * (1ull << SMP_BITS);
+  for (int j = 0; j < 64; ++j) t.p[j] = __builtin_bit_cast(smp_u64, smp_power(j) * (1ull << SMP_BITS)) - (static_cast<smp_u64>(j) << 46);
   return t;
 }
 __device__ const SamplePowers SMP_POWERS = smp_powers();
@@ -83,21 +86,27 @@ struct SampleWeight {
   double power, series;
   int k;
 };
-__device__ __forceinline__ SampleWeight smp_weight(double u, const double* powers) {
-  constexpr double L = 0.69314718055994530942 / 64.0, M = 6755399441055744.0;
+struct SampleSeries {      // of the scan, kept in registers: literals are moved there again for every token
+  double c4 = SMP_L * SMP_L * SMP_L * SMP_L / 24.0, c3 = SMP_L * SMP_L * SMP_L / 6.0, c2 = SMP_L * SMP_L / 2.0, c1 = SMP_L, whole = 4503599627370496.0;
+  static constexpr double SMP_L = 0.69314718055994530942 / 64.0;
+  __device__ __forceinline__ void keep() { asm volatile("" : "+v"(c4), "+v"(c3), "+v"(c2), "+v"(c1), "+v"(whole)); }
+};
+__device__ __forceinline__ SampleWeight smp_weight(double u, const smp_u64* powers, const SampleSeries& c) {
+  constexpr double M = 6755399441055744.0;
   const double m = u + M, r = u - (m - M);
   SampleWeight w;
   w.k = static_cast<int>(__builtin_bit_cast(smp_u64, m));
-  double p = __builtin_fma(r, L * L * L * L / 24.0, L * L * L / 6.0);
-  p = __builtin_fma(p, r, L * L / 2.0);
-  p = __builtin_fma(p, r, L);
+  double p = __builtin_fma(r, c.c4, c.c3);
+  p = __builtin_fma(p, r, c.c2);
+  p = __builtin_fma(p, r, c.c1);
   w.series = __builtin_fma(p, r, 1.0);
-  const smp_u64 t = __builtin_bit_cast(smp_u64, powers[w.k & 63]);
-  w.power = __builtin_bit_cast(double, t + (static_cast<smp_u64>(static_cast<unsigned>(w.k >> 6)) << 52));
+  const smp_u64 t = powers[w.k & 63];
+  const unsigned hi = static_cast<unsigned>(t >> 32) + (static_cast<unsigned>(w.k) << 14);
+  w.power = __builtin_bit_cast(double, (static_cast<smp_u64>(hi) << 32) | static_cast<unsigned>(t));
   return w;
 }
-__device__ __forceinline__ smp_u64 smp_whole(const SampleWeight& w) {      // the nearest whole number: the low bits of 2^52 + the weight
-  return __builtin_bit_cast(smp_u64, __builtin_fma(w.series, w.power, 4503599627370496.0)) & 0xfffffffffffffull;
+__device__ __forceinline__ smp_u64 smp_whole(const SampleWeight& w, const SampleSeries& c) {      // the nearest whole number: the low bits of 2^52 + the weight
+  return __builtin_bit_cast(smp_u64, __builtin_fma(w.series, w.power, c.whole)) & 0xfffffffffffffull;
 }
 __device__ __forceinline__ int smp_bin(int k) { return max(-k, 0) >> (6 - SMP_BIN_LOG2); }
 // larger logits first: ascending numbers, -0 with +0 (NaN has no weight and is never asked for)
@@ -161,12 +170,12 @@ __device__ __forceinline__ SampleRow smp_row(const ecospa_sample_args& q, int b)
 // ---------------------------------------------------------------------------------------------
 // scan
 // ---------------------------------------------------------------------------------------------
-template <typename T, int THREADS, int EACH>
-__global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a) {
-  constexpr int WAVES = THREADS / 64, CH = EACH / 8;
+template <typename T, int EACH>
+__global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs a) {
+  constexpr int WAVES = SMP_SCAN / 64, CH = EACH / 8;
   __shared__ smp_u64 sum[SMP_BINS];
   __shared__ unsigned count[SMP_BINS];
-  __shared__ double powers[64];
+  __shared__ smp_u64 powers[64];
   __shared__ float red_top[WAVES];
   __shared__ int red_at[WAVES], used;
   __shared__ smp_u64 total;
@@ -186,7 +195,7 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
   if (tid < 64) powers[tid] = SMP_POWERS.p[tid];
   if (tid == 0) { used = 0; total = 0; }
   if (bins) {
-    for (int i = tid; i < SMP_BINS; i += THREADS) { sum[i] = 0; count[i] = 0; }
+    for (int i = tid; i < SMP_BINS; i += SMP_SCAN) { sum[i] = 0; count[i] = 0; }
   }
   float top = -INFINITY;
 #pragma unroll
@@ -224,13 +233,15 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
   const SampleScale scale = smp_scale(top, r.c64, e);
   int most = -1;
   smp_u64 s = 0;
+  SampleSeries series;
+  series.keep();
   const auto weigh = [&](auto plain) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const SampleWeight wt = smp_weight(smp_place_as<decltype(plain)::value>(x[c][i], scale), powers);
-        const smp_u64 w = smp_whole(wt);
+        const SampleWeight wt = smp_weight(smp_place_as<decltype(plain)::value>(x[c][i], scale), powers, series);
+        const smp_u64 w = smp_whole(wt, series);
         s += w;
         if (bins && w != 0) {
           const int bin = smp_bin(wt.k);
@@ -250,7 +261,7 @@ __global__ __launch_bounds__(THREADS) void sample_scan_kernel(const SampleArgs a
   if (tid == 0) *part = SamplePart{e, total, top, 0, used, 0};
   if (bins) {
     const long long at = (static_cast<long long>(b) * a.ranges + blockIdx.x) * SMP_BINS;
-    for (int i = tid; i < used; i += THREADS) {
+    for (int i = tid; i < used; i += SMP_SCAN) {
       a.bin_sum[at + i] = sum[i];
       if (r.by_k) a.bin_count[at + i] = count[i];
     }
@@ -267,7 +278,7 @@ struct SampleShared {
   unsigned count[SMP_BINS];
   smp_u64 digit_sum[256];
   unsigned digit_count[256];
-  double powers[64];
+  smp_u64 powers[64];
   SampleScale scale[SMP_MAX_RANGES];
   int shift[SMP_MAX_RANGES], bins[SMP_MAX_RANGES];    // binades below the row's (63: no weight); histogram bins in use
   float lo[SMP_MAX_RANGES], hi[SMP_MAX_RANGES];       // logits that can fall into the bin that is looked for
@@ -446,6 +457,7 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
   const ecospa_sample_args& q = a.q;
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr int WAVES = SMP_DRAW / 64;
+  const SampleSeries series;
   const SampleRow r = smp_row(q, b);
   const SamplePart* const part = a.part + static_cast<long long>(b) * a.ranges;
   if (tid < 64) sh.powers[tid] = SMP_POWERS.p[tid];
@@ -604,8 +616,8 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
     for (int i = tid; i < min(sh.listed, SMP_LIST); i += SMP_DRAW) {
       const smp_u64 key = sh.list_key[i];
       const int g = smp_token(key) >> a.range_log2, by = sh.shift[g];
-      const SampleWeight w = smp_weight(smp_place(smp_logit(key), sh.scale[g]), sh.powers);
-      sh.list_w[i] = smp_bin(w.k) + (by << SMP_BIN_LOG2) == bin ? smp_whole(w) : 0;
+      const SampleWeight w = smp_weight(smp_place(smp_logit(key), sh.scale[g]), sh.powers, series);
+      sh.list_w[i] = smp_bin(w.k) + (by << SMP_BIN_LOG2) == bin ? smp_whole(w, series) : 0;
     }
     __syncthreads();
   };
@@ -630,8 +642,8 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
 #pragma unroll
           for (int m = 0; m < 7; ++m) y[m] = y[m + 1];
           if (!(xi >= sh.lo[g] && xi <= sh.hi[g])) continue;
-          const SampleWeight wt = smp_weight(smp_place(xi, sh.scale[g]), sh.powers);
-          const smp_u64 w = smp_whole(wt);
+          const SampleWeight wt = smp_weight(smp_place(xi, sh.scale[g]), sh.powers, series);
+          const smp_u64 w = smp_whole(wt, series);
           if ((w >> by) != 0 && smp_bin(wt.k) + (by << SMP_BIN_LOG2) == bin) f(smp_key(xi, c * SMP_CHUNK + lane * 8 + i), w, by);
         }
       });
@@ -735,12 +747,12 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const double p = smp_place(x[i], sh.scale[g]);
-      const SampleWeight wt = smp_weight(p, sh.powers);
+      const SampleWeight wt = smp_weight(p, sh.powers, series);
       const int at = smp_bin(wt.k) + (by << SMP_BIN_LOG2);
       // a token of the border's bin that weighs nothing in the row's binade is not kept: it was not counted
-      const bool kept = !cut || at < border_bin || (at == border_bin && (smp_whole(wt) >> by) != 0 && kept_there(smp_key(x[i], c * SMP_CHUNK + lane * 8 + i), p, by));
+      const bool kept = !cut || at < border_bin || (at == border_bin && (smp_whole(wt, series) >> by) != 0 && kept_there(smp_key(x[i], c * SMP_CHUNK + lane * 8 + i), p, by));
       exact[i] = wt.series * wt.power;
-      w[i] = kept ? smp_whole(wt) : 0;
+      w[i] = kept ? smp_whole(wt, series) : 0;
       s += w[i];
     }
     const smp_u64 all = smp_wave_sum(s);
@@ -773,12 +785,12 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
 // ---------------------------------------------------------------------------------------------
 // entry points
 // ---------------------------------------------------------------------------------------------
-// Ranges of 8192 tokens; of 2048 while there are few of them.
-struct SamplePlan { int threads, range_log2, ranges, chunks; };
+// Ranges of 8192 tokens; of 2048 where a row has few and the rows don't fill the card (both kernels, fp32 with top-p, us, 2048 against 8192: 1 row of 32000 21.5 : 24.4,
+// 1 of 131072 32 : 27, 64 of 32000 33.6 : 34.3, 128 of 32000 39 : 36).
+struct SamplePlan { int range_log2, ranges, chunks; };
 static SamplePlan sample_plan(int B, int V) {
   SamplePlan p;
-  const bool few = static_cast<long long>(B) * V <= 1 << 21;
-  p.threads = few ? 256 : 512;
+  const bool few = V <= 1 << 16 && static_cast<long long>(B) * V <= 1 << 21;
   p.range_log2 = few ? 11 : 13;
   p.ranges = (V + (1 << p.range_log2) - 1) >> p.range_log2;
   p.chunks = (V + SMP_CHUNK - 1) / SMP_CHUNK;
@@ -801,8 +813,8 @@ extern "C" size_t ecospa_sample_workspace_bytes(int B, int V) {
 template <typename T>
 static hipError_t sample_launch(const SampleArgs& a, const SamplePlan& p, hipStream_t st) {
   const dim3 g(p.ranges, a.q.B);
-  if (p.threads == 256) hipLaunchKernelGGL((sample_scan_kernel<T, 256, 8>), g, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((sample_scan_kernel<T, 512, 16>), g, dim3(512), 0, st, a);
+  if (p.range_log2 == 11) hipLaunchKernelGGL((sample_scan_kernel<T, 8>), g, dim3(SMP_SCAN), 0, st, a);
+  else hipLaunchKernelGGL((sample_scan_kernel<T, 32>), g, dim3(SMP_SCAN), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   static LdsAttrOnce attr_once;
