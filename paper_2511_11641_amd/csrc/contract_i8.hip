@@ -93,6 +93,8 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const QuantArgs a) {
 template <typename T>
 static void quant_launch(const QuantArgs& a, hipStream_t st) {
   const int pieces = a.cols >> 3;
+  // a workgroup a row while rows are few (64 rows of 2048: 2.9 us against 3.3 for a wavefront a row), a wavefront a row where they are many (16384 rows of 512: 6 us against
+  // 14, of 2048 16 against 26: 100 MB at 6.1 TB/s, out of the last-level cache)
   const dim3 wide(a.rows), four((a.rows + 3) / 4);
   if (a.rows <= 1024 || pieces > 64 * 8) {
     if (pieces <= 256) hipLaunchKernelGGL((quant_rows_kernel<T, 256, 1>), wide, dim3(256), 0, st, a);

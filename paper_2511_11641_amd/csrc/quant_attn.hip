@@ -63,17 +63,25 @@ __global__ __launch_bounds__(256) void quant_attn_join_kernel(const QuantAttnArg
   }
 }
 
-// Tiles of 16 queries a wavefront takes, and how many pieces the keys of a head are cut into.
+// Tiles of 16 queries a wavefront takes, and how many pieces the keys of a head are cut into.  More tiles read and convert a key less often, fewer make more
+// workgroups: as many as the rows fill while there are 512 workgroups, two a compute unit (us, heads of 64 dims, four queries' heads a key's: 64 requests of 16384
+// keys and 16 tokens, 4 : 1 tiles 192 : 251; 16 requests of 4096 and 8 tokens, 2 : 1 tiles 20.8 : 17.8.  Less than 512, here 256, costs 16 requests of 16 tokens
+// 26.5 : 21.2, more, 1024, 64 requests of 5 tokens 174 : 152).  Where one tile each leaves room, keys are cut, in no less than 512 (256: the same; 1024: one request of
+// 4096 keys 12.4 : 11.0); 1024 keys in one piece, which needs no join (one request of 1000 keys 7.8 : 10.8, of 2048 11.8 : 10.4).
+#define QA_ITEMS 512
 struct QuantPlan { int T, row_blocks, pieces, W; };
 static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {
   QuantPlan p;
   const int rows = c->h / c->h_kv * L;
   p.W = c->kp_vo <= 32 ? 2 : (c->kp_vo <= 64 ? 4 : 8);
-  p.T = rows <= 16 ? 1 : (rows <= 32 || quant_attn_tiles((c->kp_qk + 31) / 32, p.W) == 2 ? 2 : 4);
+  const long long groups = static_cast<long long>(c->B) * c->h_kv;
+  const int widest = quant_attn_tiles((c->kp_qk + 31) / 32, p.W);
+  p.T = rows <= 16 ? 1 : (rows <= 32 || widest == 2 ? 2 : 4);
+  while (p.T > 1 && groups * ((rows + 16 * p.T - 1) / (16 * p.T)) < QA_ITEMS) p.T /= 2;
   p.row_blocks = (rows + 16 * p.T - 1) / (16 * p.T);
-  const long long items = static_cast<long long>(c->B) * c->h_kv * p.row_blocks;
-  const int most = (c->own_max + 511) / 512, fill = rows > 32 ? 1024 : 512;
-  long long want = items >= fill ? 1 : (fill + items - 1) / items;
+  const long long items = groups * p.row_blocks;
+  const int most = c->own_max <= 1024 ? 1 : (c->own_max + 511) / 512;
+  long long want = items >= QA_ITEMS ? 1 : (QA_ITEMS + items - 1) / items;
   if (want > most) want = most;
   if (want < 1) want = 1;
   p.pieces = static_cast<int>(want);
@@ -117,7 +125,9 @@ extern "C" int ecospa_quant_cache_attn(ecospa_ctx* ctx, const ecospa_quant_cache
   a.scale_log2 = c->scale * 1.4426950408889634f;
   if (static_cast<long long>(c->B * c->h_kv + 7) * p.row_blocks * p.pieces > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
   const int KQ = (c->kp_qk + 31) / 32;
-  const bool once = static_cast<long long>(c->B) * c->h_kv * c->own_max * (c->kp_qk + c->kp_vo) > 96ll << 20;
+  // keys that one workgroup reads, and more of them than the last-level cache (256 MB) keeps until a next call: past the caches (64 requests of 16384 keys 132 : 138 us,
+  // 5.4 : 5.2 TB/s; out of the cache 134 MB 26 : 20)
+  const bool once = p.row_blocks == 1 && static_cast<long long>(c->B) * c->h_kv * c->own_max * (c->kp_qk + c->kp_vo) > 256ll << 20;
   const hipError_t e = p.W == 2 ? quant_attn_launch_w2(a, p.T, KQ, once, ctx->stream) : p.W == 4 ? quant_attn_launch_w4(a, p.T, KQ, once, ctx->stream) : quant_attn_launch_w8(a, p.T, KQ, once, ctx->stream);
   if (e != hipSuccess) return hip_fail(ctx, e, "quant_attn_kernel");
   if (p.pieces > 1) {
