@@ -37,7 +37,7 @@ def values(t):
 class Caches:
     """Caches of random codes and scales; rows beyond every length hold NaN, scales of blocks without a row too."""
 
-    def __init__(self, seed, Bn, h, h_kv, e, f, lens, block, cap=None, layout="heads", own_max=None, scale=0.125, powers=True):
+    def __init__(self, seed, Bn, h, h_kv, e, f, lens, block, cap=None, layout="heads", own_max=None, scale=0.125, powers=True, shared=False):
         g = gen(seed)
         self.cap = cap = max(max(lens), 1) + 3 if cap is None else cap
         codes = lambda d: (torch.randn(Bn, h_kv, cap, d, device="cuda", generator=g) * 40).clamp(-448, 448).to(F8)
@@ -46,6 +46,12 @@ class Caches:
             wide = torch.zeros(Bn, cap, h_kv, f + 16, dtype=torch.uint8, device="cuda")
             wide[..., :f] = codes(f).transpose(1, 2).view(torch.uint8)
             self.v = wide.view(F8)[..., :f].transpose(1, 2)
+        elif shared:                # one head's rows for all
+            one = lambda d: (torch.randn(1, 1, cap, d, device="cuda", generator=g) * 40).clamp(-448, 448).to(F8).view(torch.uint8)
+            k, v = one(e), one(f)
+            for t in (k, v):
+                t[:, :, max(lens):] = 0x7f
+            self.k, self.v = k.view(F8).expand(Bn, h_kv, cap, e), v.view(F8).expand(Bn, h_kv, cap, f)
         else:
             self.k, self.v = codes(e), codes(f)
         n = (cap + block - 1) // block
@@ -54,18 +60,19 @@ class Caches:
         self.k_scale, self.v_scale = scales(), scales()
         at = torch.tensor([[max(x, 0)] for x in lens], device="cuda")
         dead = torch.arange(cap, device="cuda") >= at
-        for t in (self.k, self.v):
+        for t in () if shared else (self.k, self.v):
             t.view(torch.uint8).masked_fill_(dead[:, None, :, None], 0x7f)
         unused = torch.arange(n, device="cuda") * block >= at
         self.k_scale.masked_fill_(unused[:, None], float("nan"))
         self.v_scale.masked_fill_(unused[:, None], float("nan"))
         self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
         self.B, self.h, self.h_kv, self.e, self.f, self.block, self.scale = Bn, h, h_kv, e, f, block, scale
-        self.own_max = own_max
+        self.own_max, self.shared = own_max, shared
         self.cache = B.QuantCache(self.k, self.v, self.k_scale, self.v_scale, self.lens, h, scale, block, own_max=own_max)
 
     def host(self):
-        return {"k": values(self.k), "v": values(self.v), "k_scale": values(self.k_scale), "v_scale": values(self.v_scale)}
+        n = int(self.lens.max()) if self.shared else self.cap
+        return {"k": values(self.k[:, :, :n]), "v": values(self.v[:, :, :n]), "k_scale": values(self.k_scale), "v_scale": values(self.v_scale)}
 
 
 def attend(ctx, c, L, seed, prior=False, spread=1.0):
@@ -117,6 +124,26 @@ def test_rows_around_the_tiles(ctx, rows):
 def test_pieces(ctx, n, prior):
     attend(ctx, Caches(n, 2, 4, 2, 64, 64, [n, n // 3], 64), 1, 4, prior)
     attend(ctx, Caches(n, 1, 2, 1, 96, 128, [n], 16), 3, 5, prior)
+
+
+WIDTHS = [(16, 32), (32, 48), (32, 112), (48, 16), (64, 64), (64, 128), (80, 32), (96, 64), (96, 96), (128, 32), (112, 48), (128, 128)]      # of every kernel: 32-dim steps of a key, dims of a value a lane holds
+
+
+@pytest.mark.parametrize("e,f", WIDTHS)
+@pytest.mark.parametrize("g,L", [(2, 10), (3, 15), (1, 70)])
+def test_many_rows_of_many_heads(ctx, e, f, g, L):
+    """Enough workgroups for tiles of 32 and 64 queries a wavefront, the last one not full."""
+    attend(ctx, Caches(e + f, 4, 128 * g, 128, e, f, [75, 2, 40, 33], 16), L, 9, prior=g == 2)
+
+
+@pytest.mark.parametrize("e,f", WIDTHS)
+@pytest.mark.parametrize("L", [1, 3])
+def test_caches_beyond_the_last_level_cache(ctx, e, f, L):
+    """More than 256 MB by strides and bound: all heads of all requests in the same memory."""
+    Bn, h_kv, lens = 2, 32, [300, 41]
+    c = Caches(e + f, Bn, h_kv, h_kv, e, f, lens, 64, cap=((1 << 28) // (Bn * h_kv * (e + f)) + 64) // 64 * 64 + 64, shared=True)
+    assert Bn * h_kv * c.cap * (e + f) > 1 << 28
+    attend(ctx, c, L, 10)
 
 
 def test_scales_that_are_no_powers_of_two(ctx):
