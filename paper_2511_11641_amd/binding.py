@@ -894,12 +894,21 @@ class Context:
     def ecospa_quant_rows(self, x: torch.Tensor, q: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
         """(q int8 [rows, cols], scale float32 [rows]) with x[r] ~ scale[r] * q[r]; x: [rows, cols] float32 or bf16, row stride free."""
         (rows, cols), (ld, unit) = x.shape, x.stride()
-        q = torch.empty((rows, round_up(cols, 16)), dtype=torch.int8, device=x.device)[:, :cols] if q is None else q
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device) if scale is None else scale
-        if unit != 1 or q.dtype != torch.int8 or q.shape != x.shape or q.stride(1) != 1:
-            raise ValueError(f"expected rows of {cols} dense elements, got strides {x.stride()}, {q.dtype} {tuple(q.shape)} {q.stride()}")
-        self._check(self.lib.ecospa_quant_rows(self.h, rows, cols, dtype_code(x.dtype), x.data_ptr(), ld, q.data_ptr(), q.stride(0),
-                                               _dense(scale, torch.float32, rows)), "ecospa_quant_rows")
+        if q is None:
+            q = x.new_empty((rows, cols if cols % 16 == 0 else round_up(cols, 16)), dtype=torch.int8)
+            q = q if cols % 16 == 0 else q[:, :cols]
+        elif q.dtype != torch.int8 or q.shape != x.shape or q.stride(1) != 1:
+            raise ValueError(f"expected int8 codes {tuple(x.shape)}, got {q.dtype} {tuple(q.shape)} {q.stride()}")
+        if unit != 1:
+            raise ValueError(f"expected rows of {cols} dense elements, got strides {x.stride()}")
+        if scale is None:
+            scale = x.new_empty(rows, dtype=torch.float32)
+            at_scale = scale.data_ptr()
+        else:
+            at_scale = _dense(scale, torch.float32, rows)
+        rc = self.lib.ecospa_quant_rows(self.h, rows, cols, dtype_code(x.dtype), x.data_ptr(), ld, q.data_ptr(), q.stride(0), at_scale)
+        if rc:
+            self._check(rc, "ecospa_quant_rows")
         return q, scale
 
     def ecospa_contract_quant(self, A: torch.Tensor, sa: torch.Tensor, Bm: torch.Tensor, sb: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -914,9 +923,10 @@ class Context:
             raise ValueError(f"expected int8 rows of equal length, got {A.dtype} {tuple(A.shape)} and {Bm.dtype} {tuple(Bm.shape)}")
         if out.dtype != torch.bfloat16 or out.shape != (M, width) or out.stride(1) != 1:
             raise ValueError(f"expected a bf16 output [{M}, {width}], got {out.dtype} {tuple(out.shape)}")
-        self._check(self.lib.ecospa_contract_quant(self.h, M, N, K, A.data_ptr(), lda, _dense(sa, torch.float32, M), Bm.data_ptr(), ldb,
-                                                _dense(sb, torch.float32, N), _dense(bias, torch.bfloat16, N), act, out.data_ptr(), out.stride(0)),
-                    "ecospa_contract_quant")
+        rc = self.lib.ecospa_contract_quant(self.h, M, N, K, A.data_ptr(), lda, _dense(sa, torch.float32, M), Bm.data_ptr(), ldb, _dense(sb, torch.float32, N),
+                                            _dense(bias, torch.bfloat16, N), act, out.data_ptr(), out.stride(0))
+        if rc:
+            self._check(rc, "ecospa_contract_quant")
         return out
 
     # ---- parameter update ----------------------------------------------------------------------
