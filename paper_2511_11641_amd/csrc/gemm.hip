@@ -567,7 +567,8 @@ int ecospa_gemm(ecospa_ctx* ctx, const GemmDesc& d) {
   return ECOSPA_OK;
 }
 
-// 8-bit integers: never split along K (a sum of few tokens is shared out inside the workgroups), and the choice is that of bf16 operands of as many bytes.
+// 8-bit integers: never split along K (a sum of few tokens is shared out inside the workgroups), and the choice is that of bf16 operands of as many bytes: of 66 products
+// (1 to 4096 rows, seven matrices from 1024 x 512 to 32000 x 2048) within 5 % of the fastest of the 17 kernels, 10 % where that takes 2.5 us.
 int ecospa_gemm_i8(ecospa_ctx* ctx, const GemmDesc& d) {
   if (d.trans_a || d.trans_b || d.splits > 1 || d.colsum || !((GEMM_EPIS_I8 >> d.epi.kind) & 1)) return ECOSPA_ERR_DTYPE;
   if (!gemm_i8_sa(d.epi) || !gemm_i8_sb(d.epi)) return ECOSPA_ERR_NULL;

@@ -62,7 +62,7 @@ class Server:
             if evictable and self.spare is None:  # what an eviction writes into; the cache it leaves is the next layer's
                 self.spare = (*kv(Bsz), torch.zeros((Bsz, a.h_kv, cap), dtype=torch.float32, device=dev))
         self.lm_quant = quant(stack.lm.w)
-        self._buffers, self._descs = {}, {}
+        self._buffers, self._descs, self._codes = {}, {}, {}
         self._caches()                            # without a prefix until there is one
 
     def _buf(self, name: str, rows: int, width: int, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
@@ -98,8 +98,10 @@ class Server:
         """act(x w^T + bias), by the 8-bit copy of w where there is one (act: there alone)."""
         if quant is None:
             return self.ctx.ecospa_contract(x, False, w, False, bias=bias, out=out)
-        T, K = x.shape
-        q, s = self.ctx.ecospa_quant_rows(x, self._buf("codes", T, K, torch.int8), self._buf("scales", T, 1, torch.float32))
+        codes = self._codes.get(x.shape)
+        if codes is None:
+            codes = self._codes[x.shape] = (torch.empty(x.shape, dtype=torch.int8, device="cuda"), torch.empty(x.shape[0], dtype=torch.float32, device="cuda"))
+        q, s = self.ctx.ecospa_quant_rows(x, *codes)
         return self.ctx.ecospa_contract_quant(q, s, *quant, bias=bias, act=act, out=out)
 
     def _ffn(self, f, x, quant=None):
