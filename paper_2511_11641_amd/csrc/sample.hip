@@ -108,7 +108,8 @@ __device__ __forceinline__ SampleWeight smp_weight(double u, const smp_u64* powe
 __device__ __forceinline__ smp_u64 smp_whole(const SampleWeight& w, const SampleSeries& c) {      // the nearest whole number: the low bits of 2^52 + the weight
   return __builtin_bit_cast(smp_u64, __builtin_fma(w.series, w.power, c.whole)) & 0xfffffffffffffull;
 }
-__device__ __forceinline__ int smp_bin(int k) { return max(-k, 0) >> (6 - SMP_BIN_LOG2); }
+// the bin of a place: places are 0 or less but for a rounding of 2^-6 at most (e below 10^12), so k is 0 or less
+__device__ __forceinline__ int smp_bin(int k) { return -k >> (6 - SMP_BIN_LOG2); }
 // larger logits first: ascending numbers, -0 with +0 (NaN has no weight and is never asked for)
 __device__ __forceinline__ unsigned smp_rank(float x) {
   const unsigned b = __float_as_uint(x + 0.f);
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs 
   }
   const double e = smp_binade(top, r.c64);
   const SampleScale scale = smp_scale(top, r.c64, e);
-  int most = -1;
+  int least = 1;
   smp_u64 s = 0;
   SampleSeries series;
   series.keep();
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs 
           const int bin = smp_bin(wt.k);
           atomicAdd(&sum[bin], w);
           if (r.by_k) atomicAdd(&count[bin], 1u);
-          most = max(most, bin);
+          least = min(least, wt.k);
         }
       }
     }
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs 
   else weigh(std::false_type{});
   s = smp_wave_sum(s);
   if (lane == 0) atomicAdd(&total, s);
-  if (most >= 0) atomicMax(&used, most + 1);
+  if (least <= 0) atomicMax(&used, smp_bin(least) + 1);
   __syncthreads();
   if (tid == 0) *part = SamplePart{e, total, top, 0, used, 0};
   if (bins) {
