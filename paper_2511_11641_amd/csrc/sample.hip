@@ -9,9 +9,9 @@
 //           comparisons alone, for the tokens of that bin, which go to a list in LDS; there the border is found digit by digit of (logit, index).  The histograms
 //           then say what every range keeps, hence the range that the random number falls into; only its weights are computed again.
 // Weights decide on whole tokens next to borders, so they are good to 2^-42: a table of 64 powers and four terms of the series in 64 bits, which run at the rate
-// of 32 bits here.  256 rows of 131072 fp32 logits with top-p and min-p: scan 53 us, bound by some 38 vector instructions a token (134 MB alone would be 21); draw 39 us,
-// where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps (20 us for one bf16 row of 32000 with top-k and top-p; scan 6.5).  Ranges of eight
-// tokens a lane times four wavefronts: registers for 32 logits a lane leave 4 wavefronts a SIMD, and that beats 16 (54 us) and 8 of a workgroup of 1024 (81).
+// of 32 bits here.  256 rows of 131072 fp32 logits with top-p and min-p: scan 46 us, bound by some 38 vector instructions a token (134 MB alone would be 21), and 37 without
+// a histogram; draw 39 us, where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps (20 us for one bf16
+// row of 32000 with top-k and top-p; scan 6.5).  32 logits a lane and four wavefronts a range leave 6 wavefronts a SIMD (16 logits: 50 us, of twice the wavefronts 49).
 #include "common.h"
 
 #include <type_traits>
@@ -174,8 +174,8 @@ __device__ __forceinline__ SampleRow smp_row(const ecospa_sample_args& q, int b)
 template <typename T, int EACH>
 __global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs a) {
   constexpr int WAVES = SMP_SCAN / 64, CH = EACH / 8;
-  __shared__ smp_u64 sum[SMP_BINS];
-  __shared__ unsigned count[SMP_BINS];
+  __shared__ smp_u64 sum[SMP_BINS + 64];       // behind the bins a place a lane for what weighs nothing: no branch, and no address that many lanes add to
+  __shared__ unsigned count[SMP_BINS + 64];
   __shared__ smp_u64 powers[64];
   __shared__ float red_top[WAVES];
   __shared__ int red_at[WAVES], used;
@@ -232,33 +232,42 @@ __global__ __launch_bounds__(SMP_SCAN) void sample_scan_kernel(const SampleArgs 
   }
   const double e = smp_binade(top, r.c64);
   const SampleScale scale = smp_scale(top, r.c64, e);
-  int least = 1;
   smp_u64 s = 0;
   SampleSeries series;
   series.keep();
-  const auto weigh = [&](auto plain) __attribute__((always_inline)) {
+  // mode 0: weights alone, 1: their histogram, 2: and that of counts
+  const auto weigh = [&](auto plain, auto mode) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const SampleWeight wt = smp_weight(smp_place_as<decltype(plain)::value>(x[c][i], scale), powers, series);
+        float xi = x[c][i];
+        asm volatile("" : "+v"(xi));      // its conversion stays here: made once for all modes, in front of them, it would take two registers a token
+        const SampleWeight wt = smp_weight(smp_place_as<decltype(plain)::value>(xi, scale), powers, series);
         const smp_u64 w = smp_whole(wt, series);
         s += w;
-        if (bins && w != 0) {
-          const int bin = smp_bin(wt.k);
+        if constexpr (decltype(mode)::value > 0) {
+          const int bin = w != 0 ? smp_bin(wt.k) : SMP_BINS + lane;
           atomicAdd(&sum[bin], w);
-          if (r.by_k) atomicAdd(&count[bin], 1u);
-          least = min(least, wt.k);
+          if constexpr (decltype(mode)::value > 1) atomicAdd(&count[bin], 1u);
         }
       }
     }
   };
-  if (scale.plain) weigh(std::true_type{});
-  else weigh(std::false_type{});
+  using std::integral_constant;
+  if (!scale.plain) weigh(std::false_type{}, integral_constant<int, 2>{});
+  else if (!bins) weigh(std::true_type{}, integral_constant<int, 0>{});
+  else if (r.by_k) weigh(std::true_type{}, integral_constant<int, 2>{});
+  else weigh(std::true_type{}, integral_constant<int, 1>{});
   s = smp_wave_sum(s);
   if (lane == 0) atomicAdd(&total, s);
-  if (least <= 0) atomicMax(&used, smp_bin(least) + 1);
   __syncthreads();
+  if (bins) {
+    int most = 0;
+    for (int i = tid; i < SMP_BINS; i += SMP_SCAN) most = sum[i] != 0 ? i + 1 : most;
+    if (most) atomicMax(&used, most);
+    __syncthreads();
+  }
   if (tid == 0) *part = SamplePart{e, total, top, 0, used, 0};
   if (bins) {
     const long long at = (static_cast<long long>(b) * a.ranges + blockIdx.x) * SMP_BINS;
