@@ -7,11 +7,12 @@
 //           row's later on), and a histogram of weights (and counts) in bins of a sixteenth of a binade.
 //   draw    A workgroup a row: the ranges' histograms are added and the bin with the border is found; the row is read again (it is in the last-level cache), by
 //           comparisons alone, for the tokens of that bin, which go to a list in LDS; there the border is found digit by digit of (logit, index).  The histograms
-//           then say what every range keeps, hence the range that the random number falls into; only its weights are computed again.
+//           then say what every range keeps, hence the range that the random number falls into; only its weights are computed again.  Where top-k keeps few tokens, the
+//           list takes all of them, and the rest is counted there.
 // Weights decide on whole tokens next to borders, so they are good to 2^-42: a table of 64 powers and four terms of the series in 64 bits, which run at the rate
 // of 32 bits here.  256 rows of 131072 fp32 logits with top-p and min-p: scan 46 us, bound by some 38 vector instructions a token (134 MB alone would be 21), and 37 without
-// a histogram; draw 39 us, where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps (20 us for one bf16
-// row of 32000 with top-k and top-p; scan 6.5).  32 logits a lane and four wavefronts a range leave 6 wavefronts a SIMD (16 logits: 50 us, of twice the wavefronts 49).
+// a histogram; draw 39 us, where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps.  One bf16
+// row of 32000 with a top-k of 50 and top-p: scan 6.5, draw 15, a dozen dependent steps; 20 without the list of all that top-k keeps.  32 logits a lane and four wavefronts a range leave 6 wavefronts a SIMD (16 logits: 50 us, of twice the wavefronts 49).
 #include "common.h"
 
 #include <type_traits>
@@ -460,6 +461,65 @@ __device__ __forceinline__ smp_u64 smp_border(SampleShared& sh, smp_u64 need, bo
   }
 }
 
+// the least whole number of 2^-42 at or above top_p times the weight
+__device__ __forceinline__ smp_u64 smp_share(smp_u64 weight, float top_p) {
+  const smp_u64 p = top_p > 0.f ? static_cast<smp_u64>(static_cast<double>(top_p) * 4294967296.0) : 0ull;
+  const unsigned __int128 prod = static_cast<unsigned __int128>(weight) * p;
+  return max(static_cast<smp_u64>(prod >> 32) + (static_cast<unsigned>(static_cast<smp_u64>(prod)) != 0u ? 1 : 0), 1ull);
+}
+// where a random number falls among `total`
+__device__ __forceinline__ smp_u64 smp_target(float u, smp_u64 total) {
+  if (u >= 1.f) return total - 1;
+  const smp_u64 whole = u > 0.f ? static_cast<smp_u64>(static_cast<double>(u) * 4294967296.0) : 0ull;
+  return static_cast<smp_u64>((static_cast<unsigned __int128>(total) * whole) >> 32);
+}
+// The rest of a draw whose list holds every token that top-k can keep, SMP_SHORT at most: each is counted against all others, four lanes a token, in order of
+// the logits for what is kept and in order of the vocabulary for the draw.
+__device__ __forceinline__ void smp_draw_short(SampleShared& sh, const SampleArgs& a, const SampleRow& r, int n, double least_place, int b) {
+  const ecospa_sample_args& q = a.q;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int i = tid >> 2;
+  if (tid < n) sh.digit_sum[tid] = sh.list_w[tid] >> sh.shift[smp_token(sh.list_key[tid]) >> a.range_log2];
+  if (tid == 0) { sh.out[0] = 0; sh.out[1] = 0; }
+  __syncthreads();
+  const bool mine = i < n, first = mine && (tid & 3) == 0;
+  const smp_u64 key = mine ? sh.list_key[i] : 0, w = mine ? sh.digit_sum[i] : 0;
+  const int g = smp_token(key) >> a.range_log2, by = sh.shift[g];
+  smp_u64 front = 0;
+  unsigned front_n = 0;
+  for (int m = tid & 3; m < n; m += 4) {
+    const smp_u64 x = sh.digit_sum[m];
+    const bool in = sh.list_key[m] < key && x != 0;
+    front += in ? x : 0;
+    front_n += in ? 1u : 0u;
+  }
+  front += __shfl_xor(front, 1, 64);
+  front_n += __shfl_xor(front_n, 1, 64);
+  front += __shfl_xor(front, 2, 64);
+  front_n += __shfl_xor(front_n, 2, 64);
+  bool keep = w != 0 && front_n < static_cast<unsigned>(r.k);
+  if (first && keep) atomicAdd(&sh.out[0], w);
+  __syncthreads();
+  const double place = smp_place(smp_logit(key), sh.scale[g]);
+  keep = keep && (!r.by_p || front < smp_share(sh.out[0], r.p)) && place - 64.0 * by >= least_place;
+  if (first) {
+    sh.list_w[i] = keep ? w : 0;
+    if (keep) atomicAdd(&sh.out[1], w);
+  }
+  __syncthreads();
+  const smp_u64 total = sh.out[1], target = smp_target(q.u[b], total);
+  smp_u64 before = 0;
+  for (int m = tid & 3; m < n; m += 4) before += smp_token(sh.list_key[m]) < smp_token(key) ? sh.list_w[m] : 0;
+  before += __shfl_xor(before, 1, 64);
+  before += __shfl_xor(before, 2, 64);
+  if (first && keep && before <= target && target < before + w) {
+    const SampleWeight exact = smp_weight(place, sh.powers, SampleSeries{});
+    q.token[b] = smp_token(key);
+    if (q.prob) q.prob[b] = static_cast<float>(fmin(__builtin_ldexp(exact.series * exact.power, -by) / static_cast<double>(total), 1.0));
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds_sample[];
@@ -579,8 +639,8 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
       }
     }
   };
-  // the tokens of `bin` to the list: those whose logit can be in it first, then what they weigh
-  const auto gather = [&](int bin) __attribute__((always_inline)) {
+  // the tokens of `bin` (and of those above it) to the list: those whose logit can be in it first, then what they weigh
+  const auto gather = [&](int bin, bool above) __attribute__((always_inline)) {
     if (tid == 0) sh.listed = 0;
     if (tid < a.ranges) {
       const SampleScale& s = sh.scale[tid];
@@ -592,7 +652,7 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
         if (s.plain && s.c64 > 0.0) {      // places of the bin, and a little on both sides
           const double u1 = 64.0 * by - width * bin, xl = (u1 - width - s.off) / s.c64, xh = (u1 + 1.0 - s.off) / s.c64;
           lo = static_cast<float>(xl - (__builtin_fabs(xl) * 1e-6 + 1e-36));
-          hi = bin == 0 ? INFINITY : static_cast<float>(xh + (__builtin_fabs(xh) * 1e-6 + 1e-36));
+          hi = bin == 0 || above ? INFINITY : static_cast<float>(xh + (__builtin_fabs(xh) * 1e-6 + 1e-36));
         }
       }
       sh.lo[tid] = lo;
@@ -627,7 +687,8 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
       const smp_u64 key = sh.list_key[i];
       const int g = smp_token(key) >> a.range_log2, by = sh.shift[g];
       const SampleWeight w = smp_weight(smp_place(smp_logit(key), sh.scale[g]), sh.powers, series);
-      sh.list_w[i] = smp_bin(w.k) + (by << SMP_BIN_LOG2) == bin ? smp_whole(w, series) : 0;
+      const int at = smp_bin(w.k) + (by << SMP_BIN_LOG2);
+      sh.list_w[i] = at == bin || (above && at < bin) ? smp_whole(w, series) : 0;
     }
     __syncthreads();
   };
@@ -670,13 +731,10 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
   while (phase < 3) {
     int bin = least_bin;
     smp_u64 front = 0, front_sum = 0, need = 0;
-    bool reached = true;
+    bool reached = true, few = false;
     if (phase < 2) {
-      const smp_u64 k = static_cast<smp_u64>(r.k), p = r.p > 0.f ? static_cast<smp_u64>(static_cast<double>(r.p) * 4294967296.0) : 0ull;
-      const auto of_all = [&](smp_u64 all) __attribute__((always_inline)) {      // the least whole number of 2^-42 at or above top_p times the total
-        const unsigned __int128 prod = static_cast<unsigned __int128>(bordered ? total : all) * p;
-        return max(static_cast<smp_u64>(prod >> 32) + (static_cast<unsigned>(static_cast<smp_u64>(prod)) != 0u ? 1 : 0), 1ull);
-      };
+      const smp_u64 k = static_cast<smp_u64>(r.k);
+      const auto of_all = [&](smp_u64 all) __attribute__((always_inline)) { return smp_share(bordered ? total : all, r.p); };
       const SampleFound f = phase == 0 ? smp_find(sh, SMP_BINS, [&](smp_u64) __attribute__((always_inline)) { return k; }, bin_count, bin_sum)
                                        : smp_find(sh, SMP_BINS, of_all, bin_sum, bin_count);
       bin = f.bin;
@@ -684,6 +742,7 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
       need = f.need;
       front_sum = phase == 0 ? f.front_w : front;
       reached = f.reached;
+      few = phase == 0 && reached && front + sh.count[bin] <= SMP_SHORT;
       __syncthreads();
     } else if (border_bin <= least_bin) {      // min-p cuts behind the border or in its bin, whose list is there
       break;
@@ -693,12 +752,20 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
       phase = next;
       continue;
     }
+    if (few) {      // all that top-k can keep: one list for everything that follows
+      gather(bin, true);
+      if (sh.listed <= SMP_SHORT) {
+        smp_draw_short(sh, a, r, sh.listed, least_place, b);
+        return;
+      }
+      __syncthreads();
+    }
     if (next == 2 && bin > least_bin) {      // min-p cuts in front of it: where exactly it lies doesn't matter
       border_bin = bin;
       phase = next;
       continue;
     }
-    gather(bin);
+    gather(bin, false);
     border = ~0ull;
     if (phase < 2) {
       smp_u64 taken;
@@ -739,10 +806,7 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
   if (lane == 63) sh.scan[wave] = upto;
   __syncthreads();
   const smp_u64 front = smp_waves(sh.scan, wave, total) + upto - own;
-  const float uf = q.u[b];
-  const smp_u64 u = uf > 0.f ? (uf < 1.f ? static_cast<smp_u64>(static_cast<double>(uf) * 4294967296.0) : 4294967295ull) : 0ull;
-  smp_u64 target = static_cast<smp_u64>((static_cast<unsigned __int128>(total) * u) >> 32);
-  if (uf >= 1.f) target = total - 1;
+  const smp_u64 target = smp_target(q.u[b], total);
   if (target >= front && target < front + own) {
     sh.out[0] = static_cast<smp_u64>(tid);
     sh.out[1] = (target - front) << sh.shift[tid];      // relative to the range from here on

@@ -85,6 +85,23 @@ def test_equal_logits(ctx, V):
     check(ctx, y, u, top_p=[0.51, 0.27, 0.13, 0.97, 0.73, 0.0, 0.55, 0.59, 0.22, 0.53, 0.77, 0.57])
 
 
+@pytest.mark.parametrize("n", [100, 200, 255, 256, 300])
+def test_top_k_about_what_a_list_of_all_kept_tokens_holds(ctx, n):
+    """n tokens in the border's bin, a sixteenth of a binade wide, and as many just below it, which may be taken for its own at first."""
+    x = torch.full((8, 3000), -20.0, device="cuda")
+    r = np.random.RandomState(n)
+    for b in range(8):
+        at = r.permutation(3000)
+        x[b, at[0]] = 0.0
+        x[b, at[1:n + 1]] = -65.0 / 92.332
+        x[b, at[n + 1:2 * n + 1]] = -67.8 / 92.332
+    k = [1, 2, n // 2, n, n + 1, n + 2, 2 * n, 2 * n + 1]
+    u = r.rand(8).tolist()
+    check(ctx, x, u, top_k=k)
+    check(ctx, x, u, top_k=k, top_p=[0.999, 0.3, 0.7, 0.51, 0.93, 0.77, 0.61, 0.123])
+    check(ctx, x, u, top_k=k, min_p=[0.5] * 4 + [0.49] * 4)
+
+
 def test_one_logit_far_above(ctx):
     x, r = rows(5, 8, 5000)
     x[:, 1234] = 80.0
