@@ -71,22 +71,25 @@ __global__ __launch_bounds__(THREADS) void quant_append_kernel(const QuantAppend
   const int i = id % a.touched;
   id /= a.touched;
   const int b = id / a.h_kv, head = id - b * a.h_kv;
+  const int at0 = a.cos ? a.pos[b] : 0;                                  // position of the first new token
   const int first = a.lens[b] - a.L, end = min(first + a.L, a.cap);      // rows of the new tokens
   const int blk = max(first, 0) / a.block + i, row0 = blk * a.block;
   const int lo = max(max(first, 0), row0), hi = min(end, row0 + a.block);
   if (lo >= hi) return;
   const int width = key ? a.kq : a.kv, cw = width >> 3, pieces = (hi - lo) * cw;
   const bf16_t* const src = a.qkv + a.h * a.kq + (key ? head * a.kq : a.h_kv * a.kq + head * a.kv);
-  const int pos0 = key && a.cos ? a.pos[b] - first : 0;                    // position of row 0
+  float* const at_scale = (key ? a.k_scale : a.v_scale) + (static_cast<long long>(b) * a.h_kv + head) * a.blocks + blk;
+  const bool earlier = lo > row0;
+  const float before = earlier ? *at_scale : 0.f;
   uint4 x[EACH];
   bool in[EACH];
   unsigned top = 0u;
 #pragma unroll
   for (int c = 0; c < EACH; ++c) {
-    const int p = min(c * THREADS + t, pieces - 1), r = p / cw, d = p - r * cw, at = pos0 + lo + r;
+    const int p = min(c * THREADS + t, pieces - 1), r = p / cw, d = p - r * cw, at = at0 + lo - first + r;
     in[c] = c * THREADS + t < pieces;
     x[c] = *reinterpret_cast<const uint4*>(src + (static_cast<long long>(b) * a.L + lo - first + r) * a.ld_qkv + d * 8);
-    if (a.cos) in[c] = in[c] && a.pos[b] + lo - first + r >= 0 && a.pos[b] + lo - first + r < a.L_tab;
+    if (a.cos) in[c] = in[c] && at >= 0 && at < a.L_tab;
     if (key && a.cos && in[c]) {
       const long long tab = (static_cast<long long>(head) * a.L_tab + at) * (a.kq >> 1) + d * 4;
       x[c] = quant_turn(x[c], a.cos + tab, a.sin + tab);
@@ -109,9 +112,7 @@ __global__ __launch_bounds__(THREADS) void quant_append_kernel(const QuantAppend
     for (int w = 0; w < THREADS / 64; ++w) top = max(top, red[w]);
   }
   if (top == 0u) return;      // no row of the block has an angle: nothing changes
-  float* const at_scale = (key ? a.k_scale : a.v_scale) + (static_cast<long long>(b) * a.h_kv + head) * a.blocks + blk;
-  const bool earlier = lo > row0;
-  const float before = earlier ? *at_scale : 0.f, s = fmaxf(quant_scale_for(top), before);
+  const float s = fmaxf(quant_scale_for(top), before);
   unsigned char* const dst = (key ? a.k + b * a.k_sb + head * a.k_sh : a.v + b * a.v_sb + head * a.v_sh);
   const long long st = key ? a.k_st : a.v_st;
   if (earlier && s > before) {      // the earlier rows come to the new scale
