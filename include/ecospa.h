@@ -609,7 +609,7 @@ int ecospa_logits_process(ecospa_ctx* ctx, const ecospa_logits* args /*host*/);
  * ecospa_quant_rows: scale[r] = max_c |x[r, c]| / 127 and q[r, c] = x[r, c] / scale[r] rounded to the nearest whole number (half to even), both quotients
  * those of an fp32 division, and no larger than 127 in size (a subnormal scale can be that coarse); where the scale is 0 the codes are.  A row that holds an infinity or NaN has scale NaN and zeros.  x: [rows, cols] of
  * dtype ECOSPA_F32 or ECOSPA_BF16; q: int8 [rows, cols], must not overlap x.  cols a multiple of 8; x, q 16-byte aligned, ld a multiple of 8, ld_q of 16.
- * Errors: ERR_NULL, ERR_DTYPE, ERR_SHAPE (rows < 1, cols < 8, cols % 8, a leading dimension below cols), ERR_ALIGN. */
+ * Errors: ERR_NULL, ERR_DTYPE, ERR_SHAPE (rows outside [1, 2^30], cols < 8, cols % 8, a leading dimension below cols), ERR_ALIGN. */
 int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype, const void* x, long long ld, void* q, long long ld_q, float* scale);
 
 /* C[m, n] = act( sa[m] * sb[n] * sum_k A[m, k] B[n, k] + bias[n] ), A int8 [M, K], B int8 [N, K], sums in 32-bit integers (exact), scales and what follows in

@@ -108,7 +108,7 @@ static void quant_launch(const QuantArgs& a, hipStream_t st) {
 extern "C" int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype, const void* x, long long ld, void* q, long long ld_q, float* scale) {
   if (!ctx || !x || !q || !scale) return ECOSPA_ERR_NULL;
   if (!dtype_ok(dtype)) return ECOSPA_ERR_DTYPE;
-  if (rows < 1 || cols < 8 || cols % 8 || ld < cols || ld_q < cols) return ECOSPA_ERR_SHAPE;
+  if (rows < 1 || rows > 1 << 30 || cols < 8 || cols % 8 || ld < cols || ld_q < cols) return ECOSPA_ERR_SHAPE;
   if (!aligned16(x) || !aligned16(q) || ld % 8 || ld_q % 16 || (reinterpret_cast<uintptr_t>(scale) & 3u)) return ECOSPA_ERR_ALIGN;
   QuantArgs a;
   a.x = x; a.q = static_cast<signed char*>(q); a.scale = scale; a.ld = ld; a.ld_q = ld_q; a.rows = rows; a.cols = cols;

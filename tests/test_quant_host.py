@@ -22,7 +22,7 @@ def ctx(lib):
 
 @pytest.mark.parametrize("change,code", [
     (dict(x=None), B.ERR_NULL), (dict(q=None), B.ERR_NULL), (dict(scale=None), B.ERR_NULL), (dict(dtype=2), B.ERR_DTYPE), (dict(dtype=-1), B.ERR_DTYPE),
-    (dict(rows=0), B.ERR_SHAPE), (dict(cols=0), B.ERR_SHAPE), (dict(cols=12), B.ERR_SHAPE), (dict(ld=56), B.ERR_SHAPE), (dict(ld_q=48), B.ERR_SHAPE),
+    (dict(rows=0), B.ERR_SHAPE), (dict(rows=(1 << 30) + 1), B.ERR_SHAPE), (dict(cols=0), B.ERR_SHAPE), (dict(cols=12), B.ERR_SHAPE), (dict(ld=56), B.ERR_SHAPE), (dict(ld_q=48), B.ERR_SHAPE),
     (dict(ld=68), B.ERR_ALIGN), (dict(ld_q=72), B.ERR_ALIGN), (dict(x=264), B.ERR_ALIGN), (dict(q=520), B.ERR_ALIGN),
 ], ids=str)
 def test_rows_are_refused(lib, ctx, change, code):
