@@ -219,20 +219,29 @@ void quant_attn_kernel(const QuantAttnArgs a) {
           s[t][e >> 2][e & 3] = key < sees[t] && key < key1 ? s[t][e >> 2][e & 3] : -INFINITY;
         }
     }
+    // the lane's own largest: a row's reference has to be near it, not equal to it, so the lanes of a row agree on new ones only where one falls behind
+    float top[T];
+    bool behind = false;
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-      // the lane's own largest: the row's reference has to be near it, not equal to it, so the lanes of a row agree on a new one only where it falls behind
       float most[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int e = 0; e < 8; ++e) most[e >> 2] = fmaxf(most[e >> 2], s[t][e >> 2][e & 3]);
-      const float top = fmaxf(most[0] * by[0], most[1] * by[1]);
-      if (__any(top > m[t] + QA_RESCALE)) {
-        const float up = fmaxf(m[t], qa_max4(top)), f0 = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - up);
+      top[t] = fmaxf(most[0] * by[0], most[1] * by[1]);
+      behind = behind || top[t] > m[t] + QA_RESCALE;
+    }
+    if (__any(behind)) {
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const float up = fmaxf(m[t], qa_max4(top[t])), f0 = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - up);
         m[t] = up;
         l[t] = l[t] == 0.f ? 0.f : l[t] * f0;
 #pragma unroll
         for (int f = 0; f < W; ++f) o[t][f] *= f0;
       }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
       const float ref = m[t] == -INFINITY ? 0.f : m[t];
       float p[8];
 #pragma unroll
