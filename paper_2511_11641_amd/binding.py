@@ -895,14 +895,13 @@ class Context:
         """(q int8 [rows, cols], scale float32 [rows]) with x[r] ~ scale[r] * q[r]; x: [rows, cols] float32 or bf16, row stride free."""
         (rows, cols), (ld, unit) = x.shape, x.stride()
         if q is None:
-            q = x.new_empty((rows, cols if cols % 16 == 0 else round_up(cols, 16)), dtype=torch.int8)
-            q = q if cols % 16 == 0 else q[:, :cols]
+            q = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format) if cols % 16 == 0 else x.new_empty((rows, round_up(cols, 16)), dtype=torch.int8)[:, :cols]
         elif q.dtype != torch.int8 or q.shape != x.shape or q.stride(1) != 1:
             raise ValueError(f"expected int8 codes {tuple(x.shape)}, got {q.dtype} {tuple(q.shape)} {q.stride()}")
         if unit != 1:
             raise ValueError(f"expected rows of {cols} dense elements, got strides {x.stride()}")
         if scale is None:
-            scale = x.new_empty(rows, dtype=torch.float32)
+            scale = torch.empty_strided((rows,), (1,), dtype=torch.float32, device=x.device)
             at_scale = scale.data_ptr()
         else:
             at_scale = _dense(scale, torch.float32, rows)
@@ -921,10 +920,11 @@ class Context:
         out = torch.empty((M, width), dtype=torch.bfloat16, device=A.device) if out is None else out
         if A.dtype != torch.int8 or Bm.dtype != torch.int8 or Kb != K or ua != 1 or ub != 1:
             raise ValueError(f"expected int8 rows of equal length, got {A.dtype} {tuple(A.shape)} and {Bm.dtype} {tuple(Bm.shape)}")
-        if out.dtype != torch.bfloat16 or out.shape != (M, width) or out.stride(1) != 1:
+        ldc, uc = out.stride()
+        if out.dtype != torch.bfloat16 or out.shape != (M, width) or uc != 1:
             raise ValueError(f"expected a bf16 output [{M}, {width}], got {out.dtype} {tuple(out.shape)}")
         rc = self.lib.ecospa_contract_quant(self.h, M, N, K, A.data_ptr(), lda, _dense(sa, torch.float32, M), Bm.data_ptr(), ldb, _dense(sb, torch.float32, N),
-                                            _dense(bias, torch.bfloat16, N), act, out.data_ptr(), out.stride(0))
+                                            _dense(bias, torch.bfloat16, N), act, out.data_ptr(), ldc)
         if rc:
             self._check(rc, "ecospa_contract_quant")
         return out

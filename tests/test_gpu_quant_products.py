@@ -162,3 +162,12 @@ def test_on_another_stream_and_in_a_graph(ctx):
             graph.replay()
             stream.synchronize()
             assert torch.equal(y, want)
+
+
+def test_codes_of_a_row_out_of_a_wider_matrix(ctx):
+    """A single row counts as dense whatever its stride; the codes made for it have a pitch of their own."""
+    x = _rows(4, 608, 7).cuda()
+    for part in (x[1:2, 8:520], x[1:2, :600], x[:, 8:520]):
+        q, s = ctx.ecospa_quant_rows(part)
+        wq, ws = Q.quant_rows(part.float().cpu().numpy())
+        assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws) and q.stride(0) % 16 == 0
