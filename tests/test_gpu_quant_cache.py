@@ -152,6 +152,24 @@ def test_scales_that_are_no_powers_of_two(ctx):
     attend(ctx, c, 2, 6)
 
 
+@pytest.mark.parametrize("L", [10, 20])
+def test_scales_that_are_no_powers_of_two_for_many_rows(ctx, L):
+    attend(ctx, Caches(L, 4, 256, 128, 64, 64, [75, 21, 40, 33], 16, powers=False), L, 11, prior=True)
+    attend(ctx, Caches(L, 4, 256, 128, 64, 64, [200, 9, 0, 129], 32), L, 12, spread=20.0)
+
+
+def test_keys_that_are_not_numbers_among_many_rows(ctx):
+    for L in (10, 20):
+        c = Caches(13, 4, 256, 128, 32, 32, [90] * 4, 32)
+        c.k.view(torch.uint8)[2, 77, 5, 3] = 0x7f
+        q, o, lse = rnd(gen(1), 4 * L, 256 * 32), torch.zeros(4 * L, 256 * 32, device="cuda", dtype=torch.bfloat16), torch.zeros(4, 256, L, device="cuda")
+        ctx.ecospa_quant_cache_attn(c.cache, q, o, lse=lse)
+        nan = torch.zeros(4, 256, dtype=torch.bool, device="cuda")
+        nan[2, 154:156] = True
+        assert torch.equal(lse.isnan(), nan[:, :, None].expand(4, 256, L))
+        assert torch.equal(o.view(4, L, 256, 32).isnan(), nan[:, None, :, None].expand(4, L, 256, 32))
+
+
 def test_a_bound_below_the_lengths(ctx):
     attend(ctx, Caches(5, 3, 4, 4, 32, 32, [50, 90, 20], 32, cap=100, own_max=60), 1, 7)
     attend(ctx, Caches(5, 2, 4, 4, 32, 32, [-4, 3], 32, cap=100), 5, 7, prior=True)

@@ -193,3 +193,21 @@ def test_on_another_stream_and_in_a_graph(ctx):
             graph.replay()
             stream.synchronize()
             assert torch.equal(token, want)
+
+
+@pytest.mark.parametrize("V,dtype", [(300, torch.float32), (3000, torch.bfloat16), (20000, torch.float32), (70000, torch.bfloat16)])
+def test_restrictions_together_with_temperatures_at_their_ends(ctx, V, dtype):
+    x, r = rows(V + 1, 16, V, dtype)
+    x[3, V // 3] = float("inf")
+    x[4, [5, V // 2, V - 1]] = float("inf")
+    x[5, ::2] = -float("inf")
+    x[6, : V - 40] = -float("inf")
+    x[7] *= 1e-3
+    x[8] *= 30.0
+    t = [1e-3, 1e-30, 1e30, 1.0, 0.5, 100.0, 1e-6, 1.0, 1.0, 0.02, 3e38, 1e-45, 5.0, 0.2, 2.0, 0.7]
+    for seed in range(6):
+        r = np.random.RandomState(seed + V)
+        k = [int(v) for v in np.exp(r.rand(16) * np.log(V)).astype(int)]
+        check(ctx, x, r.rand(16).tolist(), t, top_k=k, top_p=(1.0 - 0.6 * r.rand(16) ** 2).tolist(), min_p=(0.2 * r.rand(16) ** 3).tolist())
+        check(ctx, x, r.rand(16).tolist(), t, top_k=k, min_p=(10.0 ** (-8 * r.rand(16))).tolist())
+        check(ctx, x, r.rand(16).tolist(), t, top_p=r.rand(16).tolist(), min_p=(10.0 ** (-8 * r.rand(16))).tolist())
