@@ -337,3 +337,34 @@ def test_caches_on_another_stream_and_in_a_graph(ctx):
             graph.replay()
             stream.synchronize()
             assert torch.equal(o, want) and torch.equal(c.k.view(torch.uint8), after)
+
+
+@pytest.mark.parametrize("what", ["requests", "rows"])
+def test_offsets_beyond_32_bits(ctx, what):
+    """Caches whose second request, or whose rows, lie more than 4 GB apart: as the same caches side by side."""
+    Bn, h_kv, cap, e, L = 2, 2, 160, 64, 3
+    far = (1 << 32) + (1 << 20)
+    strides = (far, cap * e, e, 1) if what == "requests" else (e * h_kv, e, (1 << 25) - 64, 1)
+    size = sum((n - 1) * s for n, s in zip((Bn, h_kv, cap, e), strides)) + 1
+    assert size > 1 << 32
+    lens = torch.tensor([cap, cap - 31], dtype=torch.int32, device="cuda")
+    qkv = rnd(gen(1), Bn * (cap - 40), (4 + 2 * h_kv) * e)
+    more = rnd(gen(2), Bn * L, (4 + 2 * h_kv) * e)
+    got = []
+    for spread in (False, True):
+        k, v = ((torch.empty(size, dtype=torch.uint8, device="cuda").as_strided((Bn, h_kv, cap, e), strides) if spread else
+                 torch.empty((Bn, h_kv, cap, e), dtype=torch.uint8, device="cuda")) for _ in range(2))
+        k.fill_(0x7f), v.fill_(0x7f)
+        ks, vs = (torch.zeros((Bn, h_kv, cap // 16), device="cuda") for _ in range(2))
+        now = lens - L
+        ctx.ecospa_quant_cache_append(B.QuantCache(k.view(F8), v.view(F8), ks, vs, now, 4, 0.125, 16), qkv)
+        cache = B.QuantCache(k.view(F8), v.view(F8), ks, vs, lens, 4, 0.125, 16)
+        ctx.ecospa_quant_cache_append(cache, more)
+        k[0, :, :40], v[0, :, :40], k[1, :, :9], v[1, :, :9] = 0, 0, 0, 0      # rows in front of what was appended
+        ks.masked_fill_(ks == 0, 1.0), vs.masked_fill_(vs == 0, 1.0)
+        o, lse = torch.zeros(Bn * L, 4 * e, device="cuda", dtype=torch.bfloat16), torch.zeros(Bn, 4, L, device="cuda")
+        ctx.ecospa_quant_cache_attn(cache, more[:, :4 * e], o, lse=lse)
+        got.append((k.clone(), v.clone(), ks, vs, o, lse))
+        assert torch.isfinite(lse).all()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)

@@ -171,3 +171,23 @@ def test_codes_of_a_row_out_of_a_wider_matrix(ctx):
         q, s = ctx.ecospa_quant_rows(part)
         wq, ws = Q.quant_rows(part.float().cpu().numpy())
         assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws) and q.stride(0) % 16 == 0
+
+
+@pytest.mark.parametrize("M", [3, 300])
+def test_operands_and_results_beyond_4_gb(ctx, M):
+    """Rows of weights and of activations brought to 8 bits that lie behind the first 4 GB."""
+    N, K = 66000, 65536
+    w = torch.empty((N, K), dtype=torch.int8, device="cuda")
+    w.view(torch.int32).copy_(torch.arange(N * K // 4, device="cuda", dtype=torch.int32).view(N, K // 4).mul_(-1640531527))
+    sw, last = torch.rand(N, device="cuda") * 1e-3, N - 520
+    a, sa = ctx.ecospa_quant_rows(_rows(M, K, M).cuda())
+    y = ctx.ecospa_contract_quant(a, sa, w, sw)
+    want, slack = Q.contract_quant(a.cpu().numpy()[:4], sa.cpu().numpy()[:4], w[last:last + 40].cpu().numpy(), sw[last:last + 40].cpu().numpy())
+    got = y[:4, last:last + 40].float().cpu().numpy()
+    assert (np.abs(got - want) <= np.abs(want) * 2.0 ** -8 + slack * 2.0 ** -24 * (1 + 2.0 ** -8) + 1e-38).all()
+    del w, y
+    x = torch.zeros((40000, 65536), dtype=torch.bfloat16, device="cuda")
+    x[39990:] = _rows(10, 65536, 9).cuda()
+    q, s = ctx.ecospa_quant_rows(x)
+    wq, ws = Q.quant_rows(x[39990:].float().cpu().numpy())
+    assert np.array_equal(q[39990:].cpu().numpy(), wq) and np.array_equal(s[39990:].cpu().numpy(), ws) and not bool(s[:39990].any())
