@@ -463,17 +463,26 @@ __device__ __forceinline__ smp_u64 smp_border(SampleShared& sh, smp_u64 need, bo
   }
 }
 
-// the least whole number of 2^-42 at or above top_p times the weight
+// x p for 0 < p < 1, cut to a whole number, and whether anything was cut off: an fp32 number is 24 bits and a shift, so the product is exact in 128 bits (x < 2^63)
+__device__ __forceinline__ smp_u64 smp_times(smp_u64 x, float p, bool& more) {
+  const unsigned bits = __float_as_uint(p), e = bits >> 23;
+  const int shift = min(150 - static_cast<int>(max(e, 1u)), 127);      // 87 bits of a product: further down nothing is left
+  const unsigned __int128 prod = static_cast<unsigned __int128>(x) * ((bits & 0x7fffffu) | (e ? 0x800000u : 0u)), whole = prod >> shift;
+  more = (whole << shift) != prod;
+  return static_cast<smp_u64>(whole);
+}
+// the least whole number of 2^-42 at or above top_p < 1 times the weight, 1 at least
 __device__ __forceinline__ smp_u64 smp_share(smp_u64 weight, float top_p) {
-  const smp_u64 p = top_p > 0.f ? static_cast<smp_u64>(static_cast<double>(top_p) * 4294967296.0) : 0ull;
-  const unsigned __int128 prod = static_cast<unsigned __int128>(weight) * p;
-  return max(static_cast<smp_u64>(prod >> 32) + (static_cast<unsigned>(static_cast<smp_u64>(prod)) != 0u ? 1 : 0), 1ull);
+  if (!(top_p > 0.f)) return 1ull;
+  bool more;
+  const smp_u64 whole = smp_times(weight, top_p, more);
+  return max(whole + (more ? 1 : 0), 1ull);
 }
 // where a random number falls among `total`
 __device__ __forceinline__ smp_u64 smp_target(float u, smp_u64 total) {
   if (u >= 1.f) return total - 1;
-  const smp_u64 whole = u > 0.f ? static_cast<smp_u64>(static_cast<double>(u) * 4294967296.0) : 0ull;
-  return static_cast<smp_u64>((static_cast<unsigned __int128>(total) * whole) >> 32);
+  bool more;
+  return u > 0.f ? smp_times(total, u, more) : 0ull;
 }
 // The rest of a draw whose list holds every token that top-k can keep, SMP_SHORT at most: each is counted against all others, four lanes a token, in order of
 // the logits for what is kept and in order of the vocabulary for the draw.
