@@ -640,9 +640,9 @@ int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, l
  * ecospa_quant_cache_attn: as ecospa_prefix_attn over the own keys: query (b, t) sees the keys j < lens[b] - L + 1 + t.  o_in (bf16 [B*L, h*kp_vo], ld_oi) and lse_in
  * (float[B, h, L]): the result of attention over other keys - a shared prefix - which is joined in as ecospa_prefix_attn would have: o and lse are those over
  * all the keys; rows of o_in with lse_in = -inf are not read (both NULL: none; o may be o_in with the same ld, lse may be lse_in).  A query that sees no key has o = 0 and
- * lse = -inf; NaN and +inf scores as there.  Scales of blocks with rows are positive finite numbers (any: those that an append writes are powers of two).  A value enters its product
- * as its code times the power of two at or below its scale, which bf16 holds, a probability times what is left of the scale (1 for powers of two) rounded to bf16; lse comes from
- * the unrounded ones.
+ * lse = -inf; NaN and +inf scores as there.  Scales of blocks with rows are positive finite numbers (any, subnormal ones too: those that an append writes are powers of two; a scale of
+ * 0 makes rows of zeros).  k_scale * scale * log2 e, and 256 times the sum of a column's |v|, have to be finite in fp32.  A value enters its product as its code times the power of two
+ * at or below its scale (2^-100 for smaller ones), which bf16 holds, a probability times what is left of the scale (1 for powers of two from there on) rounded to bf16; lse comes from the unrounded ones.
  * Workspace: ecospa_quant_cache_attn_workspace_bytes (host-only query; 0 when none is needed or on bad input). */
 typedef struct {
   int B, h, h_kv, kp_qk, kp_vo;

@@ -8,8 +8,8 @@
 //   o^T = V^T P^T      A: 16 dims x 32 keys.  A lane holds W neighbouring dims of eight keys: its part of W fragments, once the bytes of two keys are
 //                      paired (a permutation instruction for two dims) and converted.  The eight keys are those whose scores the lane computed, so the
 //                      probabilities go from accumulator to operand without leaving the lane.
-// A key's scale multiplies its score.  A value's is split: its power of two goes into the conversion, exactly, and what is left (1 for the scales that an append
-// writes) into the probability.  Both are the same for 16 keys, a block or part of one.
+// A key's scale multiplies its score.  A value's is split: its power of two (2^-100 for smaller scales: bf16 then holds every code times it) goes into the conversion, exactly,
+// and what is left (1 for the scales that an append writes) into the probability.  Both are the same for 16 keys, a block or part of one.
 // Bounds.  Single tokens: memory; 64 requests, 8 heads of 64 dims, 16384 keys: 715 MB in 132 us, 5.4 TB/s (a large read here 6.35).  Prompts: vector
 // instructions, exponentials and the conversion of codes in front of 16 dense products each; 8 requests of 509 tokens, 32 heads of 64 dims on 8, over 4096 keys: 140 us,
 // 0.58 PFLOP/s.  Behind it: accumulators in vector registers alone (moves to and from the other half of the register file were a fifth of all instructions), loads that
@@ -26,6 +26,7 @@ typedef unsigned qa_uintx2 __attribute__((ext_vector_type(2)));
 
 #define QA_RESCALE 8.0f        // growth of a row's maximum, in binades, that brings its sums to the new one
 #define QA_LN2 0.6931471805599453f
+#define QA_LEAST (27u << 23)   // bits of 2^-100
 
 // two codes times the power of two below `scale` (the instruction looks at its exponent alone)
 template <bool HIGH>
@@ -181,21 +182,21 @@ void quant_attn_kernel(const QuantAttnArgs a) {
   }
   const auto step = [&](int c, const QaRaw<KQ, W>& x) __attribute__((always_inline)) {
     qa_bf16x8 vf[W];
+    const unsigned vs[2] = {__float_as_uint(x.vs[0]), __float_as_uint(x.vs[1])};
+    const float two_to[2] = {__uint_as_float(max(vs[0], QA_LEAST)), __uint_as_float(max(vs[1], QA_LEAST))};
 #pragma unroll
     for (int f = 0; f < W; f += 2) {
       unsigned w[2][4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const unsigned two = __builtin_amdgcn_perm(x.v[2 * e + 1][f >> 2], x.v[2 * e][f >> 2], f & 2 ? 0x07030602u : 0x05010400u);
-        w[0][e] = qa_pair<false>(two, x.vs[e >> 1]);
-        w[1][e] = qa_pair<true>(two, x.vs[e >> 1]);
+        w[0][e] = qa_pair<false>(two, two_to[e >> 1]);
+        w[1][e] = qa_pair<true>(two, two_to[e >> 1]);
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) vf[f + u] = __builtin_bit_cast(qa_bf16x8, qa_uintx4{w[u][0], w[u][1], w[u][2], w[u][3]});
     }
-    // what the exponents of the values' scales leave: 1 for powers of two, which is what an append writes
-    const float rest[2] = {__uint_as_float((__float_as_uint(x.vs[0]) & 0x807fffffu) | 0x3f800000u), __uint_as_float((__float_as_uint(x.vs[1]) & 0x807fffffu) | 0x3f800000u)};
-    const bool powers = rest[0] == 1.f && rest[1] == 1.f;
+    const bool powers = ((vs[0] | vs[1]) & 0x7fffffu) == 0u && min(vs[0], vs[1]) >= QA_LEAST;      // what an append writes
     qa_floatx4 s[T][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -209,7 +210,9 @@ void quant_attn_kernel(const QuantAttnArgs a) {
         for (int u = 0; u < KQ; ++u) s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u], qf[t][u], s[t][i], 0, 0, 0);
       }
     }
-    const float by[2] = {x.ks[0] * a.scale_log2, x.ks[1] * a.scale_log2};
+    // never 0, which a key's tiny scale makes: times the -inf of a masked key it would be NaN (the least number instead moves no score by 2^-21)
+    const auto positive = [](float f) __attribute__((always_inline)) { return __uint_as_float(max(__float_as_uint(f), 1u)); };
+    const float by[2] = {positive(x.ks[0] * a.scale_log2), positive(x.ks[1] * a.scale_log2)};
     if (c * 32 + 32 > sees_first) {
 #pragma unroll
       for (int t = 0; t < T; ++t)
@@ -248,6 +251,9 @@ void quant_attn_kernel(const QuantAttnArgs a) {
       for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e >> 2][e & 3], by[e >> 2], -ref));
       l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       if (!powers) {
+        float rest[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) rest[i] = vs[i] >= QA_LEAST ? __uint_as_float((vs[i] & 0x807fffffu) | 0x3f800000u) : x.vs[i] * 0x1p100f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] *= rest[e >> 2];
       }
