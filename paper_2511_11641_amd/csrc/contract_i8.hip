@@ -111,10 +111,16 @@ extern "C" int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype,
   if (rows < 1 || rows > 1 << 30 || cols < 8 || cols % 8 || ld < cols || ld_q < cols) return ECOSPA_ERR_SHAPE;
   if (!aligned16(x) || !aligned16(q) || ld % 8 || ld_q % 16 || (reinterpret_cast<uintptr_t>(scale) & 3u)) return ECOSPA_ERR_ALIGN;
   QuantArgs a;
-  a.x = x; a.q = static_cast<signed char*>(q); a.scale = scale; a.ld = ld; a.ld_q = ld_q; a.rows = rows; a.cols = cols;
-  if (dtype == ECOSPA_BF16) quant_launch<bf16_t>(a, ctx->stream);
-  else quant_launch<float>(a, ctx->stream);
-  ECOSPA_CHECK_LAUNCH(ctx, "quant_rows_kernel");
+  a.ld = ld; a.ld_q = ld_q; a.cols = cols;
+  // a launch takes fewer than 2^32 work-items, 2^24 workgroups
+  constexpr int most = 1 << 23;
+  for (int row = 0; row < rows; row += most) {
+    a.x = static_cast<const char*>(x) + row * ld * (dtype == ECOSPA_BF16 ? 2 : 4); a.q = static_cast<signed char*>(q) + row * ld_q; a.scale = scale + row;
+    a.rows = rows - row < most ? rows - row : most;
+    if (dtype == ECOSPA_BF16) quant_launch<bf16_t>(a, ctx->stream);
+    else quant_launch<float>(a, ctx->stream);
+    ECOSPA_CHECK_LAUNCH(ctx, "quant_rows_kernel");
+  }
   return ECOSPA_OK;
 }
 
