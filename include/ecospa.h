@@ -616,8 +616,8 @@ int ecospa_quant_rows(ecospa_ctx* ctx, int rows, int cols, int dtype, const void
  * fp32, C bf16, rounded once.  bias: bf16 [N] or NULL.  act: ECOSPA_ACT_NONE, a GELU, or ECOSPA_ACT_SWIGLU, where columns come in (gate, up) pairs as in a block's
  * w_1 and C is [M, N / 2], silu(gate) * up.  K a multiple of 16, N of 8 (SWIGLU: 16); A, B, C, bias and sb 16-byte aligned, lda and ldb multiples of 16,
  * ldc of 8.  Needs no workspace.
- * Errors: ERR_NULL; ERR_DTYPE (act); ERR_SHAPE (M < 1, N < 8, K outside [16, 131056], beyond which a sum could overflow; a leading dimension below its row, lda or
- * ldb of 2^24 and more, ldc of 2^23 and more); ERR_ALIGN. */
+ * Errors: ERR_NULL; ERR_DTYPE (act); ERR_SHAPE (M outside [1, 2^30], N < 8, K outside [16, 131056], beyond which a sum could overflow; a leading dimension below its row, lda or
+ * ldb of 2^24 and more, ldc of 2^23 and more; more tiles than a launch takes, from 2^24 of 256 x 256 results on in any case); ERR_ALIGN. */
 int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, long long lda, const float* sa, const void* B, long long ldb,
                        const float* sb, const void* bias, int act, void* C, long long ldc);
 
@@ -629,7 +629,7 @@ int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, l
  * ecospa_quant_cache: strides in elements (bytes), multiples of 16, at most 2^25 - 1 between rows; k, v 16-byte aligned; k_scale, v_scale dense
  * float[B, h_kv, ceil(cap / block)]; block 16, 32, 64 or 128; the other fields as ecospa_cache's.  Rows at and beyond lens[b], and scales of blocks without a row, are never
  * read, but own_max bounds lens as there.
- * Common errors, before any launch: ERR_NULL; ERR_SHAPE (as ecospa_cache's, block, B * h_kv > 65535); ERR_ALIGN; ERR_WORKSPACE.
+ * Common errors, before any launch: ERR_NULL; ERR_SHAPE (as ecospa_cache's, block, B * h_kv > 65535, more work than the 2^32 work-items of a launch); ERR_ALIGN; ERR_WORKSPACE.
  *
  * ecospa_quant_cache_append: as ecospa_cache_append (queries, positions, tables, tokens without a place).  Keys (turned, rounded to bf16) and values are stored as value / scale,
  * rounded to nearest even.  A block's scale is the least power of two, 2^-100 or more, that keeps its rows within 448, and does not fall while it has earlier rows; if it rises

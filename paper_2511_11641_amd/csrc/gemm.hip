@@ -574,11 +574,16 @@ int ecospa_gemm_i8(ecospa_ctx* ctx, const GemmDesc& d) {
   if (!gemm_i8_sa(d.epi) || !gemm_i8_sb(d.epi)) return ECOSPA_ERR_NULL;
   if (!aligned16(gemm_i8_sb(d.epi))) return ECOSPA_ERR_ALIGN;
   if (ring_wide(d)) return ECOSPA_ERR_SHAPE;
+  // a launch takes fewer than 2^32 work-items: first by the largest tiles, then by those of the choice
+  const auto fits = [&](int bm, int bn, long long threads) { return ((static_cast<long long>(d.M) + bm - 1) / bm) * ((static_cast<long long>(d.N) + bn - 1) / bn) * threads < 1ll << 32; };
+  if (d.M > 1 << 30 || !fits(256, 256, 256)) return ECOSPA_ERR_SHAPE;
   GemmDesc as_bf16 = d;
   as_bf16.dtype = ECOSPA_BF16;
   const int bad = gemm_check(as_bf16);
   if (bad) return bad;
   const int shape = ecospa_gemm_route(as_bf16);
+  if (shape >= GEMM_ROUTE_SHARE ? !fits(SHARE_SHAPES[shape - GEMM_ROUTE_SHARE].bm, SHARE_SHAPES[shape - GEMM_ROUTE_SHARE].bn, 512)
+                                : shape != GEMM_ROUTE_FLOW && !fits(RING_SHAPES[shape].bm, RING_SHAPES[shape].bn, 256)) return ECOSPA_ERR_SHAPE;
   const bool prof = prof_begin(ctx);
   const hipError_t le = shape >= GEMM_ROUTE_SHARE ? gemm_share_launch_i8(ctx, d, shape - GEMM_ROUTE_SHARE) : shape == GEMM_ROUTE_FLOW ? gemm_flow_launch_i8(ctx, d) : gemm_ring_launch_i8(ctx, d, shape);
   if (le != hipSuccess) return hip_fail(ctx, le, "gemm_i8 launch");

@@ -123,7 +123,7 @@ extern "C" int ecospa_quant_cache_attn(ecospa_ctx* ctx, const ecospa_quant_cache
   a.blocks = (c->cap + c->block - 1) / c->block;
   a.row_blocks = p.row_blocks; a.pieces = p.pieces;
   a.scale_log2 = c->scale * 1.4426950408889634f;
-  if (static_cast<long long>(c->B * c->h_kv + 7) * p.row_blocks * p.pieces > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
+  if (static_cast<long long>((c->B * c->h_kv + 7) / 8 * 8) * p.row_blocks * p.pieces * 256 >= 1ll << 32) return ECOSPA_ERR_SHAPE;      // a launch takes no more work-items
   const int KQ = (c->kp_qk + 31) / 32;
   // keys that one workgroup reads, and more of them than the last-level cache (256 MB) keeps until a next call: past the caches (64 requests of 16384 keys 132 : 138 us,
   // 5.4 : 5.2 TB/s; out of the cache 134 MB 26 : 20)

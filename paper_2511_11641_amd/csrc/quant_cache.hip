@@ -190,7 +190,7 @@ extern "C" int ecospa_quant_cache_append(ecospa_ctx* ctx, const ecospa_quant_cac
   // the block has (32 prompts of 509 tokens and 64 dims: blocks of 64, room for 2, 4 and 8 pieces a thread 39 : 43 : 56; of 128, 4 and 8 37.5 : 47)
   const int threads = pieces <= 256 ? 64 : 256;
   const long long grid = items + (a.n_queries + threads - 1) / threads;
-  if (grid > 0x7fffffffll) return ECOSPA_ERR_SHAPE;
+  if (grid * threads >= 1ll << 32) return ECOSPA_ERR_SHAPE;      // a launch takes no more work-items
   const dim3 g(static_cast<unsigned>(grid)), n(threads);
   if (pieces <= 64) hipLaunchKernelGGL((quant_append_kernel<64, 1>), g, n, 0, ctx->stream, a);
   else if (pieces <= 256) hipLaunchKernelGGL((quant_append_kernel<64, 4>), g, n, 0, ctx->stream, a);
