@@ -634,7 +634,8 @@ int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, l
  * ecospa_quant_cache_append: as ecospa_cache_append (queries, positions, tables, tokens without a place).  Keys (turned, rounded to bf16) and values are stored as value / scale,
  * rounded to nearest even.  A block's scale is the least power of two, 2^-100 or more, that keeps its rows within 448, and does not fall while it has earlier rows; if it rises
  * for a new row, the codes of the earlier ones are brought to it (exact but for those below the type's normal range).  A block that the new rows begin
- * starts anew.  Infinite elements are stored as NaN; NaN plays no part in the scale.  Earlier rows of a block belong to tokens in front of the call's: tokens are
+ * starts anew.  Earlier rows that others brought to 8 bits may have any positive scale: the new ones share it, or, where it has to rise, it becomes the power of two and every earlier
+ * code the nearest to its number.  Infinite elements are stored as NaN; NaN plays no part in the scale.  Earlier rows of a block belong to tokens in front of the call's: tokens are
  * appended in order.
  *
  * ecospa_quant_cache_attn: as ecospa_prefix_attn over the own keys: query (b, t) sees the keys j < lens[b] - L + 1 + t.  o_in (bf16 [B*L, h*kp_vo], ld_oi) and lse_in
@@ -642,7 +643,8 @@ int ecospa_contract_quant(ecospa_ctx* ctx, int M, int N, int K, const void* A, l
  * all the keys; rows of o_in with lse_in = -inf are not read (both NULL: none; o may be o_in with the same ld, lse may be lse_in).  A query that sees no key has o = 0 and
  * lse = -inf; NaN and +inf scores as there.  Scales of blocks with rows are positive finite numbers (any, subnormal ones too: those that an append writes are powers of two; a scale of
  * 0 makes rows of zeros).  k_scale * scale * log2 e, and 256 times the sum of a column's |v|, have to be finite in fp32.  A value enters its product as its code times the power of two
- * at or below its scale (2^-100 for smaller ones), which bf16 holds, a probability times what is left of the scale (1 for powers of two from there on) rounded to bf16; lse comes from the unrounded ones.
+ * at or below its scale (2^-100 for smaller ones), which bf16 holds, a probability times what is left of the scale (1 for powers of two from there on) rounded to bf16; lse
+ * comes from the unrounded ones.
  * Workspace: ecospa_quant_cache_attn_workspace_bytes (host-only query; 0 when none is needed or on bad input). */
 typedef struct {
   int B, h, h_kv, kp_qk, kp_vo;

@@ -8,7 +8,8 @@ typedef __bf16 qc_bf16x8 __attribute__((ext_vector_type(8)));
 // Append.  A workgroup takes the new rows that fall into one block of one request's keys or values of a head: its threads hold 8 dims of a row each,
 // turned in fp32 and rounded to bf16 (the value a cache of bf16 would keep), agree on the largest and write the codes.  Scales are powers of two,
 // the least that keeps the block below the type's 448, so a code is the value's own bits shifted: nothing is lost that the type can hold, and where a block's scale has to rise for a
-// new row, the codes of its earlier rows move to it exactly, but for those that fall below the normal range.  Further workgroups turn the queries.
+// new row, the codes of its earlier rows move to it exactly, but for those that fall below the normal range.  Earlier rows that others brought to 8 bits may have another scale, which
+// the new ones share unless it has to rise: quotients are divided then.  Further workgroups turn the queries.
 // Bound by memory: 32 prompts of 509 tokens, 32 query and 8 key/value heads of 64 dims, 217 MB in 39 us, 5.6 TB/s (a large copy here 5.75); single tokens by the launch.
 // ---------------------------------------------------------------------------------------------
 struct QuantAppendArgs {
@@ -42,11 +43,18 @@ __device__ __forceinline__ float quant_scale_for(unsigned bits) {
   const int e = static_cast<int>(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
   return __uint_as_float(static_cast<unsigned>(max(e, -100) + 127) << 23);
 }
-// four values times r to codes; what is not finite becomes NaN (the type has no infinity)
-__device__ __forceinline__ unsigned quant_pack4(float a, float b, float c, float d, float r) {
-  const auto put = [r](float x) __attribute__((always_inline)) { return fabsf(x) < INFINITY ? x * r : __uint_as_float(0x7fc00000u); };
+// four values, brought to a block's scale by `to`, to codes; what is not finite becomes NaN (the type has no infinity)
+template <typename F>
+__device__ __forceinline__ unsigned quant_pack4(float a, float b, float c, float d, F&& to) {
+  const auto put = [&](float x) __attribute__((always_inline)) { return fabsf(x) < INFINITY ? to(x) : __uint_as_float(0x7fc00000u); };
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(put(a), put(b), 0, false);
   return static_cast<unsigned>(__builtin_amdgcn_cvt_pk_fp8_f32(put(c), put(d), w, true));
+}
+// y, the nearest number to y + rest, as the neighbour of y + rest whose last bit is set: its rounding to a code's four bits is then that of y + rest, not that of a half way
+// which y only rounds to
+__device__ __forceinline__ float quant_sticky(float y, float rest) {
+  const unsigned u = __float_as_uint(y);
+  return y == 0.f || rest == 0.f ? y : __uint_as_float(((u ^ __float_as_uint(rest)) >> 31 ? u - 1u : u) | 1u);
 }
 template <int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS) void quant_append_kernel(const QuantAppendArgs a) {
@@ -116,7 +124,7 @@ __global__ __launch_bounds__(THREADS) void quant_append_kernel(const QuantAppend
   unsigned char* const dst = (key ? a.k + b * a.k_sb + head * a.k_sh : a.v + b * a.v_sb + head * a.v_sh);
   const long long st = key ? a.k_st : a.v_st;
   if (earlier && s > before) {      // the earlier rows come to the new scale
-    const float r = before / s;
+    const float r = before / s;      // exact: s is a power of two
     for (int p = t; p < (lo - row0) * cw; p += THREADS) {
       const int row = p / cw, d = p - row * cw;
       uint2* const at = reinterpret_cast<uint2*>(dst + (row0 + row) * st + d * 8);
@@ -125,23 +133,31 @@ __global__ __launch_bounds__(THREADS) void quant_append_kernel(const QuantAppend
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const auto f = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], false), g = __builtin_amdgcn_cvt_pk_f32_fp8(w[e], true);
-        w[e] = quant_pack4(f[0], f[1], g[0], g[1], r);
+        w[e] = quant_pack4(f[0], f[1], g[0], g[1], [r](float c) __attribute__((always_inline)) { const float y = c * r; return quant_sticky(y, __builtin_fmaf(c, r, -y)); });
       }
       *at = make_uint2(w[0], w[1]);
     }
   }
   if (THREADS > 64) __syncthreads();      // everyone has read the scale of before
   if (t == 0) *at_scale = s;
-  const float r = 1.f / s;
+  const auto store = [&](auto&& to) __attribute__((always_inline)) {
 #pragma unroll
-  for (int c = 0; c < EACH; ++c) {
-    if (!in[c]) continue;
-    const int p = c * THREADS + t, row = p / cw, d = p - row * cw;
-    const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-    float f[8];
+    for (int c = 0; c < EACH; ++c) {
+      if (!in[c]) continue;
+      const int p = c * THREADS + t, row = p / cw, d = p - row * cw;
+      const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+      float f[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(w[e] << 16); f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
-    *reinterpret_cast<uint2*>(dst + (lo + row) * st + d * 8) = make_uint2(quant_pack4(f[0], f[1], f[2], f[3], r), quant_pack4(f[4], f[5], f[6], f[7], r));
+      for (int e = 0; e < 4; ++e) { f[2 * e] = __uint_as_float(w[e] << 16); f[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+      *reinterpret_cast<uint2*>(dst + (lo + row) * st + d * 8) = make_uint2(quant_pack4(f[0], f[1], f[2], f[3], to), quant_pack4(f[4], f[5], f[6], f[7], to));
+    }
+  };
+  if ((__float_as_uint(s) & 0x7fffffu) == 0u) {      // a power of two, exactly
+    const float r = 1.f / s;
+    store([r](float v) __attribute__((always_inline)) { return v * r; });
+  } else {      // (both scaled by 2^64 where s is small, so that no remainder is lost below the least number)
+    const float up = s < 1.f ? 0x1p64f : 1.f, d = s * up;
+    store([up, d](float v) __attribute__((always_inline)) { const float n = v * up, y = n / d; return quant_sticky(y, __builtin_fmaf(-y, d, n)); });
   }
 }
 
