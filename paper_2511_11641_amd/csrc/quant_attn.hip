@@ -66,8 +66,9 @@ __global__ __launch_bounds__(256) void quant_attn_join_kernel(const QuantAttnArg
 // Tiles of 16 queries a wavefront takes, and how many pieces the keys of a head are cut into.  More tiles read and convert a key less often, fewer make more
 // workgroups: as many as the rows fill while there are 512 workgroups, two a compute unit (us, heads of 64 dims, four queries' heads a key's: 64 requests of 16384
 // keys and 16 tokens, 4 : 1 tiles 192 : 251; 16 requests of 4096 and 8 tokens, 2 : 1 tiles 20.8 : 17.8.  Less than 512, here 256, costs 16 requests of 16 tokens
-// 26.5 : 21.2, more, 1024, 64 requests of 5 tokens 174 : 152).  Where one tile each leaves room, keys are cut, in no less than 512 (256: the same; 1024: one request of
-// 4096 keys 12.4 : 11.0); 1024 keys in one piece, which needs no join (one request of 1000 keys 7.8 : 10.8, of 2048 11.8 : 10.4).
+// 26.5 : 21.2, more, 1024, 64 requests of 5 tokens 174 : 152).  Where one tile each leaves room, keys are cut, into a piece for each 512 that a request may hold (256: the
+// same; 1024: one request of 4096 keys 12.4 : 11.0), which a request's own keys then share in whole 128s; 1024 keys in one piece, which needs no join (one request of 1000 keys
+// 7.8 : 10.8, of 2048 11.8 : 10.4).
 #define QA_ITEMS 512
 struct QuantPlan { int T, row_blocks, pieces, W; };
 static QuantPlan quant_plan(const ecospa_quant_cache* c, int L) {

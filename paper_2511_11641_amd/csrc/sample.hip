@@ -27,7 +27,10 @@ typedef unsigned long long smp_u64;
 #define SMP_BINS ((SMP_LEAST >> (6 - SMP_BIN_LOG2)) + 4)
 #define SMP_CHUNK 512                    // tokens of a chunk: 8 a lane
 #define SMP_MAX_V (1 << 20)              // 42 bits of a weight and 20 of a vocabulary: sums below 2^63
-#define SMP_MAX_RANGES 512
+#define SMP_RANGE_LOG2 13                // tokens of a range: 8192, or
+#define SMP_FEW_LOG2 11                  // 2048 where a row has few (sample_plan), SMP_FEW_V at most
+#define SMP_FEW_V (1 << 16)
+#define SMP_MAX_RANGES 128
 #define SMP_LIST 4096
 #define SMP_SHORT 256
 #define SMP_SCAN 256
@@ -118,7 +121,7 @@ __device__ __forceinline__ unsigned smp_rank(float x) {
   const unsigned b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? b : 0x7fffffffu - b;
 }
-// sums over the wavefront, v < 2^45: two halves through lane permutations
+// sums over the wavefront, v < 2^51 (a lane of the scan adds up 32 tokens, 2^47 at most): two parts through lane permutations, whose sums of 64 lanes stay below 2^32
 __device__ __forceinline__ unsigned smp_add64(unsigned v) {
 #define SMP_DPP(ctrl) v += static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), (ctrl), 0xF, 0xF, true))
   SMP_DPP(0xB1); SMP_DPP(0x4E); SMP_DPP(0x141); SMP_DPP(0x140);
@@ -302,6 +305,7 @@ struct SampleShared {
 };
 static_assert(sizeof(SampleShared) <= 120 * 1024, "LDS of a compute unit");
 static_assert(SMP_BINS <= SMP_DRAW, "a bin a thread");
+static_assert(SMP_MAX_V >> SMP_RANGE_LOG2 <= SMP_MAX_RANGES && SMP_FEW_V >> SMP_FEW_LOG2 <= SMP_MAX_RANGES && SMP_MAX_RANGES <= SMP_DRAW, "ranges of a row");
 // running sums over the lanes of a wavefront, by lane permutations; ROWS: over every 16 lanes
 template <int CTRL, int ROW_MASK>
 __device__ __forceinline__ smp_u64 smp_moved(smp_u64 v) {      // 0 where a lane has no source
@@ -875,8 +879,8 @@ __global__ __launch_bounds__(SMP_DRAW) void sample_draw_kernel(const SampleArgs 
 struct SamplePlan { int range_log2, ranges, chunks; };
 static SamplePlan sample_plan(int B, int V) {
   SamplePlan p;
-  const bool few = V <= 1 << 16 && static_cast<long long>(B) * V <= 1 << 21;
-  p.range_log2 = few ? 11 : 13;
+  const bool few = V <= SMP_FEW_V && static_cast<long long>(B) * V <= 1 << 21;
+  p.range_log2 = few ? SMP_FEW_LOG2 : SMP_RANGE_LOG2;
   p.ranges = (V + (1 << p.range_log2) - 1) >> p.range_log2;
   p.chunks = (V + SMP_CHUNK - 1) / SMP_CHUNK;
   return p;
@@ -898,7 +902,7 @@ extern "C" size_t ecospa_sample_workspace_bytes(int B, int V) {
 template <typename T>
 static hipError_t sample_launch(const SampleArgs& a, const SamplePlan& p, hipStream_t st) {
   const dim3 g(p.ranges, a.q.B);
-  if (p.range_log2 == 11) hipLaunchKernelGGL((sample_scan_kernel<T, 8>), g, dim3(SMP_SCAN), 0, st, a);
+  if (p.range_log2 == SMP_FEW_LOG2) hipLaunchKernelGGL((sample_scan_kernel<T, 8>), g, dim3(SMP_SCAN), 0, st, a);
   else hipLaunchKernelGGL((sample_scan_kernel<T, 32>), g, dim3(SMP_SCAN), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
