@@ -253,8 +253,10 @@ def main(argv=None):
     ap.add_argument("--cache-block", type=int, choices=(16, 32, 64, 128), help="own caches in 8-bit floats, a scale for this many rows; all own tokens are kept")
     ap.add_argument("--quant-weights", action="store_true", help="weights in 8-bit integers")
     ap.add_argument("--top-p", type=float, help="draw tokens from this share of the probability instead of taking the best")
-    ap.add_argument("--temperature", type=float, default=1.0, help="of the draw")
+    ap.add_argument("--temperature", type=float, help="of the draw (1)")
     a = ap.parse_args(argv)
+    if a.temperature is not None and a.top_p is None:
+        ap.error("--temperature is that of a draw: give --top-p (1 draws from all tokens)")
     from .synth import CONFIGS
     cfg = dict(CONFIGS["c3_llama1b_layer"], B=1, L=64)
     st = DecoderStack(B.Context("cuda:0"), cfg, a.layers, 32000, keep=(1, 2), train=False)
@@ -268,7 +270,7 @@ def main(argv=None):
     draw = {}
     if a.top_p is not None:
         each = lambda x: torch.full((a.batch,), x, device="cuda")
-        draw = dict(u=torch.rand((a.steps, a.batch), device="cuda", generator=gen), top_p=each(a.top_p), temperature=each(a.temperature))
+        draw = dict(u=torch.rand((a.steps, a.batch), device="cuda", generator=gen), top_p=each(a.top_p), temperature=each(1.0 if a.temperature is None else a.temperature))
     for timed in (False, True):
         srv.set_prefix(prefix)
         torch.cuda.synchronize()
