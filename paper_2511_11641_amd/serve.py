@@ -213,7 +213,8 @@ class Server:
         ``Context.ecospa_logits_process``: repetition, frequency, presence, temperature, bias_ids, bias, mask, mask_row); the
         history of the penalties is the prompt and what came since.  Full caches are cut down to `keep` keys.  -> int32 [Bsz, steps]; -1
         where no token was left to pick (everything masked, or not a number), and token 0 is fed in its place.
-        u (float32 [steps, Bsz], in [0, 1)): tokens are drawn by these numbers instead, from what top_k (int32), top_p and min_p (each [Bsz] or None) leave."""
+        u (float32 [steps, Bsz], in [0, 1)): tokens are drawn by these numbers instead, from what top_k (int32), top_p and min_p (each [Bsz] or None) leave;
+        all of them on the GPU."""
         if u is None and not (top_k is None and top_p is None and min_p is None):
             raise ValueError("top_k, top_p and min_p restrict a draw: give its random numbers u")
         Bsz, L = prompts.shape
@@ -221,6 +222,8 @@ class Server:
             if u.shape != (steps, Bsz) or u.dtype != torch.float32:
                 raise ValueError(f"expected random numbers float32 [{steps}, {Bsz}], got {u.dtype} {tuple(u.shape)}")
             u, T = u.contiguous(), control.pop("temperature", None)      # the draw's own: its weights come from unrounded logits
+            if not all(t is None or t.is_cuda for t in (u, T, top_k, top_p, min_p)):
+                raise ValueError("random numbers and what restricts a draw have to be on the GPU")
             wide = self._buf("wide", Bsz, B.round_up(self.st.vocab, 8), torch.float32)[:, :self.st.vocab]
         self._room(L + max(steps - 1, 0))         # the last token is not fed
         history = torch.zeros((Bsz, L + steps), dtype=torch.int32, device="cuda")
