@@ -10,9 +10,9 @@
 //                      probabilities go from accumulator to operand without leaving the lane.
 // A key's scale multiplies its score.  A value's is split: its power of two (2^-100 for smaller scales: bf16 then holds every code times it) goes into the conversion, exactly,
 // and what is left (1 for the scales that an append writes) into the probability.  Both are the same for 16 keys, a block or part of one.
-// Bounds.  Single tokens: memory; 64 requests, 8 heads of 64 dims, 16384 keys: 715 MB in 132 us, 5.4 TB/s (a large read here 6.35).  Prompts: vector
-// instructions, exponentials and the conversion of codes in front of 16 dense products each; 8 requests of 509 tokens, 32 heads of 64 dims on 8, over 4096 keys: 140 us,
-// 0.58 PFLOP/s.  Behind it: accumulators in vector registers alone (moves to and from the other half of the register file were a fifth of all instructions), loads that
+// Bounds.  Single tokens: memory; 64 requests, 8 heads of 64 dims, 16384 keys: 715 MB in 131 to 136 us, 5.3 to 5.4 TB/s (a large read here 6.35).  Prompts: vector
+// instructions, exponentials and the conversion of codes in front of 16 dense products each; 8 requests of 509 tokens, 32 heads of 64 dims on 8, over 4096 keys: 140 to 146 us,
+// 0.56 to 0.58 PFLOP/s.  Behind it: accumulators in vector registers alone (moves to and from the other half of the register file were a fifth of all instructions), loads that
 // are asked for without branches.
 #pragma once
 #include "quant_cache.h"

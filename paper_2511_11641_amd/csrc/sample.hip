@@ -11,7 +11,7 @@
 //           list takes all of them, and the rest is counted there.
 // Weights decide on whole tokens next to borders, so they are good to 2^-42: a table of 64 powers and four terms of the series in 64 bits, which run at the rate
 // of 32 bits here.
-// 256 rows of 131072 fp32 logits with top-p and min-p: scan 46 us, bound by 33 vector instructions a token, the unit 82 % busy (134 MB alone would be 21); draw 39 us,
+// 256 rows of 131072 fp32 logits with top-p and min-p: scan 46 us, bound by 33 vector instructions a token, the unit 82 % busy (134 MB alone would be 21); draw 40 us,
 // where every row is read again from the last-level cache at up to 11 TB/s and the rest is some 20 dependent steps.  One bf16 row of 32000 with a top-k of 50 and top-p:
 // scan 6.5, draw 15, a dozen dependent steps; 20 without the list of all that top-k keeps.  32 logits a lane and four wavefronts a range leave 6 wavefronts a SIMD
 // (16 logits 50 us, eight wavefronts 49).
